@@ -10,6 +10,9 @@
  *   qarvd_quant_act         online:  gather-permute + per-token dynamic symmetric INT8
  *   qarvd_w8a8_dual_gemm    online:  INT8xINT8->INT32 on MFMA, two accumulators, fp32 dequant + bias
  *
+ * Beside them stand the linear's fused endings (activation, gate, residual: qarvd_dual_gemm_fused) and what follows the q / k / v
+ * projections (head norms and the rotation by position: qarvd_qk_norm_rope).
+ *
  * Conventions
  *   - Every pointer is DEVICE memory unless its comment says "host".  The caller owns every
  *     buffer; the library allocates nothing.  The only state it keeps between calls is what it
@@ -289,6 +292,97 @@ qarvd_status qarvd_w8a8_dual_gemm_q8(const int8_t *Xq, int64_t ldxq, const float
                                      int32_t K, int32_t K_o, qarvd_act act, float out_scale,
                                      int8_t *Y8, int64_t ldy8, int32_t variant, void *stream);
 int32_t qarvd_q8_gemm_num_variants(void);
+
+/*
+ * Fused ending of a quantized linear: activation, gate and residual applied in the GEMM's epilogue,
+ *     y      = the fp32 result of qarvd_w8a8_dual_gemm (same arithmetic, bias included)
+ *     a      = y, or gelu_tanh(y) as defined above
+ *     Y[m,n] = fmaf(gate[m / gate_rows, n], a, residual[m,n])     stored as fp32, or rounded to bf16 once
+ * A missing residual is +0, a missing gate 1; with neither, Y is `a` itself.  GELU is evaluated in fp32 with one hardware 2^t and
+ * one hardware reciprocal per value; it lies within 4e-7 + 2e-6 |gelu(y)| of the real-valued function.
+ *   act        QARVD_ACT_NONE or QARVD_ACT_GELU_TANH
+ *   gate       in  f32 [groups, ldg] or NULL: tokens m with the same m / gate_rows share a row (one modulation vector per frame:
+ *              gate_rows = its tokens); the last group may be shorter.  gate_rows >= 1; gate_rows >= M: one row, ldg is ignored
+ *   residual   in  [M, ldr] of Y's type or NULL.  It may be Y itself (same address and stride): every element is read before it
+ *              is written.  Any other overlap of Y with an input is undefined
+ * The fastest kernels need what they need of Y, and a 16-byte aligned gate with ldg % 4 == 0, a residual aligned to four of its
+ * elements with ldr % 4 == 0, ldg and ldr of at most 2^20; anything else runs on general tiles.
+ */
+typedef struct {
+    qarvd_act act;
+    int32_t gate_rows;
+    const float *gate;
+    int64_t ldg;
+    const void *residual;
+    int64_t ldr;
+} qarvd_ending;
+
+/*
+ * qarvd_w8a8_dual_gemm (w_bits 8) or qarvd_w4a8_dual_gemm (w_bits 4) with a fused ending; `ending` is HOST memory, NULL = none.
+ * variant: 0 = heuristic, 1..qarvd_fused_gemm_num_variants() pick a kernel; one that cannot run the call (the other w_bits among
+ * the reasons) returns QARVD_ERR_UNSUPPORTED.  Fully asynchronous on `stream`.
+ */
+qarvd_status qarvd_dual_gemm_fused(const int8_t *Xq, int64_t ldxq, const float *s_x, int32_t w_bits, const void *Wq, int64_t ldwq,
+                                   const float *s_normal, const float *s_outlier, const float *bias, const qarvd_ending *ending,
+                                   int32_t M, int32_t N, int32_t K, int32_t K_o, void *Y, qarvd_dtype ydt, int64_t ldy,
+                                   int32_t variant, void *stream);
+int32_t qarvd_fused_gemm_num_variants(void);
+
+/* qarvd_linear with a fused ending: same workspace, same checks, nothing launched before all of them. */
+qarvd_status qarvd_linear_fused(const void *X, qarvd_dtype xdt, int64_t ldx, const int32_t *perm, int32_t w_bits, const void *Wq,
+                                int64_t ldwq, const float *s_normal, const float *s_outlier, const float *bias,
+                                const qarvd_ending *ending, int32_t M, int32_t N, int32_t K, int32_t K_o, void *Y, qarvd_dtype ydt,
+                                int64_t ldy, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Norm of queries and keys and their rotation by position, in one pass over both (what follows the q / k / v projections):
+ *     NORM_HEAD  x <- x / sqrt(mean(x^2 over the head's D channels) + eps) * weight[d]
+ *     NORM_ROW   x <- x / sqrt(mean(x^2 over all heads of the token) + eps) * weight[h * D + d]
+ *     rotation   pair i of a head, (x[2i], x[2i+1]) (interleaved) or (x[i], x[i + R/2]), turns by the angle
+ *                pos[m, axis(i)] * freq[i];  R = rotary channels, the sum of axis_dims; channels from R on keep their value
+ * Pairs belong to the axes in their order: the first axis_dims[0] / 2 to axis 0, the next to axis 1 ... (time, height, width).
+ * Sums, statistics and the rotation are fp32, the angle is reduced in fp64 (positions of any int32 size), and the result is
+ * rounded to the tensors' type once.
+ *   qarvd_heads  one of the two tensors: element d of head h of token m at x[m * ld + h * head_stride + d], out likewise.
+ *                weight f32, NULL = ones.  Token-major (ld >= (heads - 1) * head_stride + D) or head-major (head_stride >=
+ *                (M - 1) * ld + D).  out may be x (same address and strides); any other overlap is undefined
+ *   q, k         HOST structs; k may be NULL (queries alone); heads may differ (shared keys)
+ *   norm, eps    QARVD_NORM_*; eps >= 0
+ *   rope         HOST struct, NULL = no rotation.  pos i32 [M, ldpos] on the device, n_axes columns (1 to 3); freq f64 [R/2] on the
+ *                device, radians per unit of position; axis_dims even and positive, R <= D
+ * D <= 512.  Tensors aligned to their elements; the fastest kernel needs D % 8 == 0, 16-byte aligned tensors and strides that are
+ * multiples of 16 bytes (and R % 8 == 0 unless interleaved).  Fully asynchronous on `stream`.
+ */
+typedef enum { QARVD_NORM_NONE = 0, QARVD_NORM_HEAD = 1, QARVD_NORM_ROW = 2 } qarvd_norm;
+typedef struct {
+    const void *x;
+    int64_t ld, head_stride;
+    void *out;
+    int64_t ld_out, head_stride_out;
+    const float *weight;
+    int32_t heads;
+} qarvd_heads;
+typedef struct {
+    const int32_t *pos;
+    int64_t ldpos;
+    const double *freq;
+    int32_t n_axes;
+    int32_t axis_dims[3];
+    int32_t interleaved;
+} qarvd_rope;
+qarvd_status qarvd_qk_norm_rope(const qarvd_heads *q, const qarvd_heads *k, qarvd_dtype dt, int32_t M, int32_t D, qarvd_norm norm,
+                                float eps, const qarvd_rope *rope, void *stream);
+
+/*
+ * The q / k / v projection as one layer, ready for attention: qarvd_linear into Y [M, ldy] whose columns are
+ * [heads_q * D queries | heads_k * D keys | the rest (values)], then qarvd_qk_norm_rope on the queries and keys in place.
+ * N >= (heads_q + heads_k) * D; heads_k may be 0.  Queries and keys are rounded to Y's type between the two, as by the two calls.
+ */
+qarvd_status qarvd_linear_qkv(const void *X, qarvd_dtype xdt, int64_t ldx, const int32_t *perm, int32_t w_bits, const void *Wq,
+                              int64_t ldwq, const float *s_normal, const float *s_outlier, const float *bias, int32_t M, int32_t N,
+                              int32_t K, int32_t K_o, int32_t heads_q, int32_t heads_k, int32_t D, qarvd_norm norm,
+                              const float *weight_q, const float *weight_k, float eps, const qarvd_rope *rope, void *Y,
+                              qarvd_dtype ydt, int64_t ldy, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * Same operation with the kernel variant chosen by the caller instead of the built-in

@@ -34,6 +34,21 @@ class _DetectCfg(C.Structure):
                 ("forced_mask", C.c_void_p)]
 
 
+class _Ending(C.Structure):
+    _fields_ = [("act", C.c_int), ("gate_rows", C.c_int32), ("gate", C.c_void_p), ("ldg", C.c_int64), ("residual", C.c_void_p),
+                ("ldr", C.c_int64)]
+
+
+class _Heads(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("ld", C.c_int64), ("head_stride", C.c_int64), ("out", C.c_void_p), ("ld_out", C.c_int64),
+                ("head_stride_out", C.c_int64), ("weight", C.c_void_p), ("heads", C.c_int32)]
+
+
+class _Rope(C.Structure):
+    _fields_ = [("pos", C.c_void_p), ("ldpos", C.c_int64), ("freq", C.c_void_p), ("n_axes", C.c_int32), ("axis_dims", C.c_int32 * 3),
+                ("interleaved", C.c_int32)]
+
+
 def lib_path() -> Path:
     return _LIB_PATH
 
@@ -96,6 +111,19 @@ def load_library():
     lib.qarvd_w8a8_dual_gemm_q8.restype = C.c_int
     lib.qarvd_q8_gemm_num_variants.argtypes = []
     lib.qarvd_q8_gemm_num_variants.restype = i32
+    lib.qarvd_dual_gemm_fused.argtypes = [vp, i64, vp, i32, vp, i64, vp, vp, vp, C.POINTER(_Ending), i32, i32, i32, i32, vp, C.c_int, i64,
+                                          i32, vp]
+    lib.qarvd_dual_gemm_fused.restype = C.c_int
+    lib.qarvd_fused_gemm_num_variants.argtypes = []
+    lib.qarvd_fused_gemm_num_variants.restype = i32
+    lib.qarvd_linear_fused.argtypes = [vp, C.c_int, i64, vp, i32, vp, i64, vp, vp, vp, C.POINTER(_Ending), i32, i32, i32, i32, vp, C.c_int,
+                                       i64, vp, C.c_size_t, vp]
+    lib.qarvd_linear_fused.restype = C.c_int
+    lib.qarvd_qk_norm_rope.argtypes = [C.POINTER(_Heads), C.POINTER(_Heads), C.c_int, i32, i32, C.c_int, f32, C.POINTER(_Rope), vp]
+    lib.qarvd_qk_norm_rope.restype = C.c_int
+    lib.qarvd_linear_qkv.argtypes = [vp, C.c_int, i64, vp, i32, vp, i64, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, C.c_int, vp, vp, f32,
+                                     C.POINTER(_Rope), vp, C.c_int, i64, vp, C.c_size_t, vp]
+    lib.qarvd_linear_qkv.restype = C.c_int
     lib.qarvd_gemm_num_variants.argtypes = []
     lib.qarvd_gemm_num_variants.restype = i32
     lib.qarvd_gemm_variant_name.argtypes = [i32]
@@ -443,4 +471,218 @@ def w8a8_linear(X: torch.Tensor, w: DualScaleWeight, bias: Optional[torch.Tensor
                           w.s_normal.data_ptr(), w.s_outlier.data_ptr(), _ptr(bias), M, w.N, K, K_o, Y.data_ptr(), _dt(Y),
                           w.N, ws.data_ptr(), need, _stream(stream))
     _check(st, "qarvd_linear")
+    return Y
+
+
+# ---- fused endings --------------------------------------------------------------------------------------------
+
+def fused_gemm_num_variants() -> int:
+    return int(load_library().qarvd_fused_gemm_num_variants())
+
+
+def _on_call_device(stream, *tensors):
+    """A kernel runs on the current device, or the given stream's: its tensors have to be there."""
+    index = torch._C._cuda_getDevice() if stream is None else stream.device_index if hasattr(stream, "device_index") else stream.device.index
+    for t in tensors:
+        if t is not None and t.get_device() != index:
+            raise ValueError("a tensor is on %s, the call on device %d" % (t.device, index))
+
+
+def _f32(t: Optional[torch.Tensor], what: str):
+    if t is not None and t.dtype != torch.float32:
+        raise TypeError("%s must be float32" % what)
+
+
+def _vector(t: Optional[torch.Tensor], n: int, what: str):
+    _f32(t, what)
+    if t is not None and (t.shape != (n,) or (n > 1 and t.stride(0) != 1)):
+        raise ValueError("%s must be a contiguous vector of %d" % (what, n))
+
+
+def _ending(M: int, N: int, act: int, gate, gate_rows, residual, dtype) -> Optional[_Ending]:
+    """Checks of the ending's tensors against the output's shape and type, and the C struct."""
+    e = _Ending(int(act), M, None, N, None, N)
+    if gate is not None:
+        _f32(gate, "gate")
+        if gate.dim() not in (1, 2) or gate.shape[-1] != N or (N > 1 and gate.stride(-1) != 1):
+            raise ValueError("gate must be [N] or [groups, N] with unit inner stride")
+        groups = gate.shape[0] if gate.dim() == 2 else 1
+        if gate_rows is None:
+            if groups == 0 or M % groups:
+                raise ValueError("%d tokens in %d groups: give gate_rows" % (M, groups))
+            gate_rows = M // groups
+        if gate_rows < 1 or groups * gate_rows < M:
+            raise ValueError("%d groups of %d tokens do not cover %d" % (groups, gate_rows, M))
+        e.gate, e.gate_rows, e.ldg = gate.data_ptr(), min(gate_rows, M), gate.stride(0) if gate.dim() == 2 else N
+    elif gate_rows is not None:
+        raise ValueError("gate_rows without a gate")
+    if residual is not None:
+        if residual.dtype != dtype:
+            raise TypeError("residual is %s, the output %s" % (residual.dtype, dtype))
+        if residual.shape != (M, N) or (N > 1 and residual.stride(1) != 1):
+            raise ValueError("residual must be [M, N] with unit inner stride")
+        e.residual, e.ldr = residual.data_ptr(), max(residual.stride(0), N) if M == 1 else residual.stride(0)
+    return e
+
+
+def _out(Y, M: int, N: int, dtype, device, stream):
+    """The output: the caller's, checked, or a new one."""
+    if Y is None:
+        return _empty((M, N), dtype, device, stream)
+    if Y.shape != (M, N) or (N > 1 and Y.stride(1) != 1):
+        raise ValueError("Y must be [M, N] with unit inner stride")
+    return Y
+
+
+def _ld(t: torch.Tensor) -> int:
+    """Row stride; a single row's says nothing."""
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+def w8a8_dual_gemm_fused(Xq: torch.Tensor, s_x: torch.Tensor, w: DualScaleWeight, bias: Optional[torch.Tensor], M: int, act: int = ACT_NONE,
+                         gate: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, gate_rows: Optional[int] = None,
+                         out_dtype=torch.bfloat16, Y: Optional[torch.Tensor] = None, variant: int = 0, stream=None) -> torch.Tensor:
+    """qarvd_dual_gemm_fused: Y = residual + gate * act(dual GEMM + bias), INT8 or INT4 weights.  gate f32 [N], or [groups, N] for groups of
+    gate_rows tokens (M / groups unless given); residual [M, N] of Y's type; Y may be the residual."""
+    lib = load_library()
+    dtype = out_dtype if Y is None else Y.dtype
+    e = _ending(M, w.N, act, gate, gate_rows, residual, dtype)
+    _on_call_device(stream, Xq, s_x, w.Wq, gate, residual, Y)
+    Y = _out(Y, M, w.N, dtype, Xq.device, stream)
+    st = lib.qarvd_dual_gemm_fused(_ptr(Xq), Xq.stride(0), _ptr(s_x), w.bits, _ptr(w.Wq), w.Wq.stride(0), _ptr(w.s_normal), _ptr(w.s_outlier),
+                                   _ptr(bias), C.byref(e), M, w.N, w.K, w.K_o, _ptr(Y), _dt(Y), _ld(Y), variant, _stream(stream))
+    _check(st, "qarvd_dual_gemm_fused")
+    return Y
+
+
+def w8a8_linear_fused(X: torch.Tensor, w: DualScaleWeight, bias: Optional[torch.Tensor], act: int = ACT_NONE, gate: Optional[torch.Tensor] = None,
+                      residual: Optional[torch.Tensor] = None, gate_rows: Optional[int] = None, out_dtype=torch.bfloat16,
+                      Y: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """qarvd_linear_fused: quant_act followed by w8a8_dual_gemm_fused in one call."""
+    lib = load_library()
+    _dev2d(X, "X")
+    M, K = X.shape
+    if K != w.K:
+        raise ValueError("X has %d channels, the layer %d" % (K, w.K))
+    dtype = out_dtype if Y is None else Y.dtype
+    e = _ending(M, w.N, act, gate, gate_rows, residual, dtype)
+    _on_call_device(stream, X, w.Wq, gate, residual, Y)
+    need = lib.qarvd_linear_workspace(M, K, w.K_o)
+    ws = _empty(need, torch.uint8, X.device, stream, scratch=True)
+    Y = _out(Y, M, w.N, dtype, X.device, stream)
+    st = lib.qarvd_linear_fused(_ptr(X), _dt(X), _ld(X), _ptr(w.perm), w.bits, _ptr(w.Wq), w.Wq.stride(0), _ptr(w.s_normal), _ptr(w.s_outlier),
+                                _ptr(bias), C.byref(e), M, w.N, K, w.K_o, _ptr(Y), _dt(Y), _ld(Y), _ptr(ws), need, _stream(stream))
+    _check(st, "qarvd_linear_fused")
+    return Y
+
+
+# ---- norm and rotation of queries and keys -----------------------------------------------------------------------
+
+NORM_NONE, NORM_HEAD, NORM_ROW = 0, 1, 2
+
+
+def rope_frequencies(axis_dims, theta: float = 10000.0, device="cuda") -> torch.Tensor:
+    """f64 [sum(axis_dims) / 2]: theta^(-2 i / d) for the pairs of each axis of d channels, radians per unit of position."""
+    return torch.cat([float(theta) ** (-torch.arange(0, d, 2, dtype=torch.float64) / d) for d in axis_dims]).to(device)
+
+
+@dataclass
+class Rope:
+    """The rotation of a model's heads: channels of each axis (up to three: time, height, width), the pairs' frequencies and their layout."""
+    axis_dims: tuple
+    freq: torch.Tensor         # f64 [sum(axis_dims) / 2] on the device (rope_frequencies)
+    interleaved: bool = True   # pairs (2i, 2i + 1); otherwise (i, i + R/2)
+
+
+def _rope(rope: Optional[Rope], pos: Optional[torch.Tensor], M: int) -> Optional[_Rope]:
+    if rope is None:
+        if pos is not None:
+            raise ValueError("positions without a rope")
+        return None
+    n, half = len(rope.axis_dims), sum(rope.axis_dims) // 2
+    if not 1 <= n <= 3:
+        raise ValueError("one to three axes, not %d" % n)
+    if pos is None or pos.dtype != torch.int32:
+        raise TypeError("pos must be int32")
+    if pos.dim() == 1 and n == 1:
+        pos = pos.unsqueeze(1)
+    if pos.shape != (M, n) or (n > 1 and pos.stride(1) != 1):
+        raise ValueError("pos must be [M, %d] with unit inner stride" % n)
+    if rope.freq.dtype != torch.float64:
+        raise TypeError("rope.freq must be float64")
+    if rope.freq.shape != (half,) or (half > 1 and rope.freq.stride(0) != 1):
+        raise ValueError("rope.freq must be a contiguous vector of %d" % half)
+    return _Rope(pos.data_ptr(), pos.stride(0), rope.freq.data_ptr(), n, (C.c_int32 * 3)(*rope.axis_dims), int(bool(rope.interleaved)))
+
+
+def _norm_weight(w, norm: int, heads: int, D: int, what: str):
+    if w is not None and norm == NORM_NONE:
+        raise ValueError("%s without a norm" % what)
+    _vector(w, heads * D if norm == NORM_ROW else D, what)
+
+
+def _heads(x: torch.Tensor, out: torch.Tensor, w) -> _Heads:
+    return _Heads(x.data_ptr(), x.stride(0), x.stride(1), out.data_ptr(), out.stride(0), out.stride(1), _ptr(w), x.shape[1])
+
+
+def _check_heads(x: torch.Tensor, what: str, like=None):
+    if not x.is_cuda or x.dim() != 3 or (x.shape[2] > 1 and x.stride(2) != 1):
+        raise ValueError("%s must be a [tokens, heads, channels] device tensor with unit inner stride" % what)
+    if like is not None and (x.shape != like.shape or x.dtype != like.dtype):
+        raise ValueError("%s must have the shape and type of what it is the output of" % what)
+
+
+def qk_norm_rope(Q: torch.Tensor, K: Optional[torch.Tensor], norm: int = NORM_HEAD, weight_q: Optional[torch.Tensor] = None,
+                 weight_k: Optional[torch.Tensor] = None, eps: float = 1e-6, pos: Optional[torch.Tensor] = None, rope: Optional[Rope] = None,
+                 out_q: Optional[torch.Tensor] = None, out_k: Optional[torch.Tensor] = None, stream=None):
+    """qarvd_qk_norm_rope: RMS norm of each head (or a token's whole row) and rotation by `pos` int32 [M, axes].  Q [M, heads, D], K [M, heads_k, D] or
+    None, f32 / bf16, any token and head strides.  Returns the outputs: out_q, out_k (Q and K themselves for in place) or new dense tensors."""
+    lib = load_library()
+    _check_heads(Q, "Q")
+    M, hq, D = Q.shape
+    _norm_weight(weight_q, norm, hq, D, "weight_q")
+    r = _rope(rope, pos, M)
+    if K is None:
+        if weight_k is not None or out_k is not None:
+            raise ValueError("weight_k or out_k without K")
+    else:
+        _check_heads(K, "K")
+        if K.shape[0] != M or K.shape[2] != D or K.dtype != Q.dtype:
+            raise ValueError("Q and K must have the same tokens, channels and type")
+        _norm_weight(weight_k, norm, K.shape[1], D, "weight_k")
+    for o, x, what in ((out_q, Q, "out_q"), (out_k, K, "out_k")):
+        if o is not None:
+            _check_heads(o, what, x)
+    _on_call_device(stream, Q, K, weight_q, weight_k, pos, rope and rope.freq, out_q, out_k)
+    if out_q is None:
+        out_q = _empty((M, hq, D), Q.dtype, Q.device, stream)
+    if K is not None and out_k is None:
+        out_k = _empty(tuple(K.shape), K.dtype, K.device, stream)
+    st = lib.qarvd_qk_norm_rope(C.byref(_heads(Q, out_q, weight_q)), None if K is None else C.byref(_heads(K, out_k, weight_k)), _dt(Q), M, D,
+                                int(norm), eps, None if r is None else C.byref(r), _stream(stream))
+    _check(st, "qarvd_qk_norm_rope")
+    return out_q, out_k
+
+
+def w8a8_linear_qkv(X: torch.Tensor, w: DualScaleWeight, bias: Optional[torch.Tensor], heads_q: int, heads_k: int, head_dim: int,
+                    norm: int = NORM_HEAD, weight_q: Optional[torch.Tensor] = None, weight_k: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                    pos: Optional[torch.Tensor] = None, rope: Optional[Rope] = None, out_dtype=torch.bfloat16, stream=None) -> torch.Tensor:
+    """qarvd_linear_qkv: the fused q / k / v projection with its queries and keys normed and rotated.  Returns Y [M, N], columns
+    [heads_q * head_dim | heads_k * head_dim | values]."""
+    lib = load_library()
+    _dev2d(X, "X")
+    M, K = X.shape
+    if K != w.K:
+        raise ValueError("X has %d channels, the layer %d" % (K, w.K))
+    _norm_weight(weight_q, norm, heads_q, head_dim, "weight_q")
+    _norm_weight(weight_k, norm, heads_k, head_dim, "weight_k")
+    r = _rope(rope, pos, M)
+    _on_call_device(stream, X, w.Wq, weight_q, weight_k, pos, rope and rope.freq)
+    need = lib.qarvd_linear_workspace(M, K, w.K_o)
+    ws = _empty(need, torch.uint8, X.device, stream, scratch=True)
+    Y = _empty((M, w.N), out_dtype, X.device, stream)
+    st = lib.qarvd_linear_qkv(_ptr(X), _dt(X), _ld(X), _ptr(w.perm), w.bits, _ptr(w.Wq), w.Wq.stride(0), _ptr(w.s_normal), _ptr(w.s_outlier),
+                              _ptr(bias), M, w.N, K, w.K_o, heads_q, heads_k, head_dim, int(norm), _ptr(weight_q), _ptr(weight_k), eps,
+                              None if r is None else C.byref(r), _ptr(Y), _dt(Y), w.N, _ptr(ws), need, _stream(stream))
+    _check(st, "qarvd_linear_qkv")
     return Y

@@ -156,10 +156,12 @@ qarvd_status check_and_fill(int bits, const int8_t *Xq, int64_t ldxq, const floa
          reinterpret_cast<uintptr_t>(dbg_acc_outlier)) & 3u)
         return QARVD_ERR_UNSUPPORTED;
     GemmArgs g;
+    g.K = K; g.K_o = K_o;
     g.Xq = Xq; g.Wq = reinterpret_cast<const int8_t *>(Wq); g.s_x = s_x; g.s_n = s_normal; g.s_o = s_outlier; g.bias = bias;
     g.Y = Y; g.dbg_n = dbg_acc_normal; g.dbg_o = dbg_acc_outlier;
     g.ldxq = ldxq; g.ldwq = ldwq; g.ldy = ldy; g.M = M; g.N = N; g.n_off = pk.n_off; g.kp = pk.kp;
     g.tiles_m = g.tiles_n = 0; g.act = 0; g.out_scale = 0.0f; g.store_wt = 0;
+    g.gate = nullptr; g.R = nullptr; g.ldg = g.ldr = 0; g.gate_rows = 0x7fffffff;
     g.vec_out = vector_out_ok(g, ydt);
     *out = g;
     return QARVD_OK;
@@ -305,10 +307,12 @@ extern "C" qarvd_status qarvd_w8a8_dual_gemm_q8(const int8_t *Xq, int64_t ldxq, 
     if ((N % 16) || !qarvd_aligned16(Y8) || (ldy8 % 16) || ldxq > (1 << 22) || ldwq > (1 << 22) || ldy8 > (1 << 22))
         return QARVD_ERR_UNSUPPORTED;
     GemmArgs g;
+    g.K = K; g.K_o = K_o;
     g.Xq = Xq; g.Wq = Wq; g.s_x = s_x; g.s_n = s_normal; g.s_o = s_outlier; g.bias = bias;
     g.Y = Y8; g.dbg_n = nullptr; g.dbg_o = nullptr;
     g.ldxq = ldxq; g.ldwq = ldwq; g.ldy = ldy8; g.M = M; g.N = N; g.n_off = pk.n_off; g.kp = pk.kp;
     g.tiles_m = g.tiles_n = 0; g.act = (int32_t)act; g.out_scale = out_scale; g.vec_out = 1; g.store_wt = 0;
+    g.gate = nullptr; g.R = nullptr; g.ldg = g.ldr = 0; g.gate_rows = 0x7fffffff;
     if (g.n_off > 128) return QARVD_ERR_UNSUPPORTED;
     if (variant == 0) {
         const double T = g.kp / 64;
@@ -326,6 +330,105 @@ extern "C" qarvd_status qarvd_w8a8_dual_gemm_q8(const int8_t *Xq, int64_t ldxq, 
     return (g.n_off > 0 ? v.dual : v.single)(g, reinterpret_cast<hipStream_t>(stream));
 }
 
+// ---- fused endings: activation, gate and residual in the epilogue ----------------------------------------------
+namespace {
+struct FusedVariant {
+    int BM, BN, bits;
+    int form;           // of the W4 variants: 0 aligned and an outlier block of at most 128 bytes, 1 strides up to 2^22, 2 anything
+    double c, a, b;     // cost model of pick_variant
+    qarvd_status (*launch)(const GemmArgs &, qarvd_dtype, hipStream_t);
+};
+// The tiles and cost constants of the plain GEMMs: an ending adds to a tile's epilogue what it adds to every other's.
+const FusedVariant kFusedVariants[] = {
+    {256, 256, 8, 0, 0.50, 7.85, 0.539, launch_dma128_fused<256, 256, 2, 4, 2, false, false>},
+    {256, 128, 8, 0, 0.60, 5.81, 0.314, launch_dma128_fused<256, 128, 4, 2, 3, false, false>},
+    {128, 256, 8, 0, 0.55, 5.40, 0.333, launch_dma128_fused<128, 256, 2, 4, 3, false, false>},
+    {128, 128, 8, 0, 1.30, 3.60, 0.183, launch_dma128_fused<128, 128, 2, 4, 3, false, false>},
+    {64, 128, 8, 0, 1.91, 2.35, 0.157, launch_dma128_fused<64, 128, 2, 4, 4, false, false>},
+    {64, 64, 8, 0, 2.40, 0.77, 0.083, launch_dma128_fused<64, 64, 2, 2, 4, false, false>},
+    {128, 128, 8, 1, 1.69, 4.01, 0.181, launch_dma128_fused<128, 128, 2, 4, 3, true, false>},
+    {64, 128, 8, 1, 1.62, 2.97, 0.131, launch_dma128_fused<64, 128, 2, 4, 4, true, false>},
+    {64, 64, 8, 1, 3.13, 0.98, 0.088, launch_dma128_fused<64, 64, 2, 2, 4, true, false>},
+    {128, 128, 8, 2, 0, 0, 0, launch_staged_fused<false>},
+    {256, 256, 4, 0, 2.80, 8.00, 0.517, launch_dma128_fused<256, 256, 2, 4, 3, false, true>},
+    {256, 128, 4, 0, 1.59, 4.44, 0.366, launch_dma128_fused<256, 128, 4, 2, 3, false, true>},
+    {128, 256, 4, 0, 1.29, 4.79, 0.357, launch_dma128_fused<128, 256, 2, 4, 3, false, true>},
+    {128, 128, 4, 1, 2.74, 3.47, 0.196, launch_dma128_fused<128, 128, 2, 4, 3, true, true>},
+    {64, 64, 4, 1, 3.60, 1.00, 0.101, launch_dma128_fused<64, 64, 2, 2, 3, true, true>},
+    {128, 128, 4, 2, 0, 0, 0, launch_staged_fused<true>},
+};
+constexpr int kNumFusedVariants = sizeof(kFusedVariants) / sizeof(kFusedVariants[0]);
+
+// Checks of an ending beside those of the GEMM, and its part of the kernel arguments.  vec_out then covers the residual and the gate too.
+qarvd_status fill_ending(const qarvd_ending *e, qarvd_dtype ydt, GemmArgs *g)
+{
+    if (!e) return QARVD_OK;
+    if (e->act != QARVD_ACT_NONE && e->act != QARVD_ACT_GELU_TANH) return QARVD_ERR_INVALID_ARG;
+    const size_t esz = ydt == QARVD_F32 ? 4 : 2;
+    if (e->gate) {
+        if (e->gate_rows <= 0 || (e->gate_rows < g->M && e->ldg < g->N)) return QARVD_ERR_INVALID_ARG;
+        if (reinterpret_cast<uintptr_t>(e->gate) & 3u) return QARVD_ERR_UNSUPPORTED;
+        g->gate = e->gate;
+        g->gate_rows = e->gate_rows;
+        g->ldg = e->gate_rows < g->M ? e->ldg : 0;            // one group: its row alone
+        g->vec_out = g->vec_out && qarvd_aligned16(e->gate) && g->ldg % 4 == 0 && g->ldg <= (1 << 20);
+    }
+    if (e->residual) {
+        if (e->ldr < g->N) return QARVD_ERR_INVALID_ARG;
+        if (reinterpret_cast<uintptr_t>(e->residual) % esz) return QARVD_ERR_UNSUPPORTED;
+        g->R = e->residual;
+        g->ldr = e->ldr;
+        g->vec_out = g->vec_out && (reinterpret_cast<uintptr_t>(e->residual) & (4 * esz - 1)) == 0 && e->ldr % 4 == 0 && e->ldr <= (1 << 20);
+    }
+    g->act = (int32_t)e->act;
+    return QARVD_OK;
+}
+
+qarvd_status launch_fused(int bits, int32_t variant, const GemmArgs &g, qarvd_dtype ydt, void *stream)
+{
+    if (variant == 0) {
+        // Nothing behind the sum: the plain GEMM's own kernels.
+        if (!g.gate && !g.R && g.act == QARVD_ACT_NONE) {
+            if (bits == 4)
+                return qarvd_w4a8_dual_gemm(g.Xq, g.ldxq, g.s_x, reinterpret_cast<const uint8_t *>(g.Wq), g.ldwq, g.s_n, g.s_o, g.bias, g.M, g.N,
+                                            g.K, g.K_o, g.Y, ydt, g.ldy, nullptr, nullptr, 0, stream);
+            return qarvd_w8a8_dual_gemm(g.Xq, g.ldxq, g.s_x, g.Wq, g.ldwq, g.s_n, g.s_o, g.bias, g.M, g.N, g.K, g.K_o, g.Y, ydt, g.ldy, nullptr,
+                                        nullptr, stream);
+        }
+        const bool fast_ok = g.n_off <= 128 && g.vec_out;
+        // (INT4: the any-width tiles stand beside the aligned ones, as for the plain GEMM)
+        const int form = !short_rows_ok(g) ? 2 : fast_ok ? 0 : 1;
+        Cand cand[kNumFusedVariants];
+        int n = 0;
+        for (int i = 0; i < kNumFusedVariants; ++i) {
+            const FusedVariant &v = kFusedVariants[i];
+            if (v.bits == bits && (v.form == form || (bits == 4 && form == 0 && v.form == 1))) cand[n++] = {i + 1, v.BM, v.BN, v.c, v.a, v.b};
+        }
+        variant = cheapest(cand, n, g);
+    }
+    const FusedVariant &v = kFusedVariants[variant - 1];
+    if (v.bits != bits || (v.form == 0 && !(g.n_off <= 128 && g.vec_out)) || (v.form == 1 && !short_rows_ok(g))) return QARVD_ERR_UNSUPPORTED;
+    return v.launch(g, ydt, reinterpret_cast<hipStream_t>(stream));
+}
+}  // namespace
+
+extern "C" int32_t qarvd_fused_gemm_num_variants(void) { return kNumFusedVariants; }
+
+extern "C" qarvd_status qarvd_dual_gemm_fused(const int8_t *Xq, int64_t ldxq, const float *s_x, int32_t w_bits, const void *Wq, int64_t ldwq,
+                                              const float *s_normal, const float *s_outlier, const float *bias, const qarvd_ending *ending,
+                                              int32_t M, int32_t N, int32_t K, int32_t K_o, void *Y, qarvd_dtype ydt, int64_t ldy,
+                                              int32_t variant, void *stream)
+{
+    if ((w_bits != 8 && w_bits != 4) || variant < 0 || variant > kNumFusedVariants) return QARVD_ERR_INVALID_ARG;
+    GemmArgs g;
+    if (qarvd_status s_c = check_and_fill(w_bits, Xq, ldxq, s_x, Wq, ldwq, s_normal, s_outlier, bias, M, N, K, K_o, Y, ydt, ldy, nullptr,
+                                          nullptr, &g);
+        s_c != QARVD_OK)
+        return s_c;
+    if (qarvd_status s_e = fill_ending(ending, ydt, &g); s_e != QARVD_OK) return s_e;
+    return launch_fused(w_bits, variant, g, ydt, stream);
+}
+
 // ---- the online pair in one call ------------------------------------------------------------------------------
 // Workspace: Xq [M, packed_ld] | s_x [M]; packed_ld is a multiple of 128, so both are aligned.
 extern "C" size_t qarvd_linear_workspace(int32_t M, int32_t K, int32_t K_o)
@@ -334,10 +437,13 @@ extern "C" size_t qarvd_linear_workspace(int32_t M, int32_t K, int32_t K_o)
     return M > 0 && ld > 0 ? (size_t)M * (size_t)ld + (size_t)M * sizeof(float) : 0;
 }
 
-extern "C" qarvd_status qarvd_linear(const void *X, qarvd_dtype xdt, int64_t ldx, const int32_t *perm, int32_t w_bits,
-                                     const void *Wq, int64_t ldwq, const float *s_normal, const float *s_outlier,
-                                     const float *bias, int32_t M, int32_t N, int32_t K, int32_t K_o, void *Y,
-                                     qarvd_dtype ydt, int64_t ldy, void *workspace, size_t workspace_bytes, void *stream)
+namespace {
+// The quantizer into the workspace, and the arguments of the GEMM on it.  Both halves' arguments are checked before the first of
+// them is launched: the GEMM's (and the ending's) here, quant_act's by itself.
+qarvd_status quantize_for_gemm(const void *X, qarvd_dtype xdt, int64_t ldx, const int32_t *perm, int32_t w_bits, const void *Wq, int64_t ldwq,
+                               const float *s_normal, const float *s_outlier, const float *bias, const qarvd_ending *ending, int32_t M,
+                               int32_t N, int32_t K, int32_t K_o, void *Y, qarvd_dtype ydt, int64_t ldy, void *workspace,
+                               size_t workspace_bytes, void *stream, GemmArgs *g)
 {
     const size_t need = qarvd_linear_workspace(M, K, K_o);
     if (need == 0 || (w_bits != 8 && w_bits != 4)) return QARVD_ERR_INVALID_ARG;
@@ -345,18 +451,64 @@ extern "C" qarvd_status qarvd_linear(const void *X, qarvd_dtype xdt, int64_t ldx
     const int64_t ld = qarvd_packed_ld(K, K_o);
     int8_t *const Xq = reinterpret_cast<int8_t *>(workspace);
     float *const s_x = reinterpret_cast<float *>(Xq + (size_t)M * (size_t)ld);
-    // Both halves' arguments are checked before the first of them is launched: the GEMM's here, quant_act's by itself.
-    GemmArgs g;
     if (qarvd_status s_c = check_and_fill(w_bits, Xq, ld, s_x, Wq, ldwq, s_normal, s_outlier, bias, M, N, K, K_o, Y, ydt, ldy, nullptr,
-                                          nullptr, &g);
+                                          nullptr, g);
         s_c != QARVD_OK)
         return s_c;
-    const size_t gemm_bytes = (size_t)N * ((size_t)g.kp * w_bits / 8 + (size_t)M * (ydt == QARVD_F32 ? 4 : 2));
-    if (qarvd_status st = qarvd_quant_act_before_gemm(X, xdt, M, K, ldx, K_o > 0 ? perm : nullptr, K_o, Xq, ld, s_x, gemm_bytes, stream); st != QARVD_OK)
+    if (qarvd_status s_e = fill_ending(ending, ydt, g); s_e != QARVD_OK) return s_e;
+    const size_t y_bytes = (size_t)M * (ydt == QARVD_F32 ? 4 : 2);
+    const size_t gemm_bytes = (size_t)N * ((size_t)g->kp * w_bits / 8 + y_bytes * (g->R ? 2 : 1));
+    return qarvd_quant_act_before_gemm(X, xdt, M, K, ldx, K_o > 0 ? perm : nullptr, K_o, Xq, ld, s_x, gemm_bytes, stream);
+}
+}  // namespace
+
+extern "C" qarvd_status qarvd_linear(const void *X, qarvd_dtype xdt, int64_t ldx, const int32_t *perm, int32_t w_bits,
+                                     const void *Wq, int64_t ldwq, const float *s_normal, const float *s_outlier,
+                                     const float *bias, int32_t M, int32_t N, int32_t K, int32_t K_o, void *Y,
+                                     qarvd_dtype ydt, int64_t ldy, void *workspace, size_t workspace_bytes, void *stream)
+{
+    GemmArgs g;
+    if (qarvd_status st = quantize_for_gemm(X, xdt, ldx, perm, w_bits, Wq, ldwq, s_normal, s_outlier, bias, nullptr, M, N, K, K_o, Y, ydt, ldy,
+                                            workspace, workspace_bytes, stream, &g);
+        st != QARVD_OK)
         return st;
     if (w_bits == 4)
-        return qarvd_w4a8_dual_gemm(Xq, ld, s_x, reinterpret_cast<const uint8_t *>(Wq), ldwq, s_normal, s_outlier, bias, M, N, K, K_o,
+        return qarvd_w4a8_dual_gemm(g.Xq, g.ldxq, g.s_x, reinterpret_cast<const uint8_t *>(Wq), ldwq, s_normal, s_outlier, bias, M, N, K, K_o,
                                     Y, ydt, ldy, nullptr, nullptr, 0, stream);
-    return qarvd_w8a8_dual_gemm_variant(0, Xq, ld, s_x, reinterpret_cast<const int8_t *>(Wq), ldwq, s_normal, s_outlier, bias, M, N, K,
+    return qarvd_w8a8_dual_gemm_variant(0, g.Xq, g.ldxq, g.s_x, reinterpret_cast<const int8_t *>(Wq), ldwq, s_normal, s_outlier, bias, M, N, K,
                                         K_o, Y, ydt, ldy, nullptr, nullptr, stream);
+}
+
+extern "C" qarvd_status qarvd_linear_fused(const void *X, qarvd_dtype xdt, int64_t ldx, const int32_t *perm, int32_t w_bits, const void *Wq,
+                                           int64_t ldwq, const float *s_normal, const float *s_outlier, const float *bias,
+                                           const qarvd_ending *ending, int32_t M, int32_t N, int32_t K, int32_t K_o, void *Y,
+                                           qarvd_dtype ydt, int64_t ldy, void *workspace, size_t workspace_bytes, void *stream)
+{
+    GemmArgs g;
+    if (qarvd_status st = quantize_for_gemm(X, xdt, ldx, perm, w_bits, Wq, ldwq, s_normal, s_outlier, bias, ending, M, N, K, K_o, Y, ydt, ldy,
+                                            workspace, workspace_bytes, stream, &g);
+        st != QARVD_OK)
+        return st;
+    return launch_fused(w_bits, 0, g, ydt, stream);
+}
+
+// ---- q / k / v projection, head norms and rotation ----------------------------------------------------------------
+extern "C" qarvd_status qarvd_linear_qkv(const void *X, qarvd_dtype xdt, int64_t ldx, const int32_t *perm, int32_t w_bits, const void *Wq,
+                                         int64_t ldwq, const float *s_normal, const float *s_outlier, const float *bias, int32_t M, int32_t N,
+                                         int32_t K, int32_t K_o, int32_t heads_q, int32_t heads_k, int32_t D, qarvd_norm norm,
+                                         const float *weight_q, const float *weight_k, float eps, const qarvd_rope *rope, void *Y,
+                                         qarvd_dtype ydt, int64_t ldy, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (heads_q <= 0 || heads_k < 0 || D <= 0 || ((int64_t)heads_q + heads_k) * D > N || ldy < N || !Y) return QARVD_ERR_INVALID_ARG;
+    const size_t esz = ydt == QARVD_F32 ? 4 : 2;
+    char *const keys = reinterpret_cast<char *>(Y) + (size_t)heads_q * D * esz;
+    const qarvd_heads q = {Y, ldy, D, Y, ldy, D, weight_q, heads_q};
+    const qarvd_heads k = {keys, ldy, D, keys, ldy, D, weight_k, heads_k};
+    // checked before the linear launches anything, which checks the rest
+    if (qarvd_status st = qarvd_heads_check(&q, heads_k ? &k : nullptr, ydt, M, D, norm, eps, rope); st != QARVD_OK) return st;
+    if (qarvd_status st = qarvd_linear(X, xdt, ldx, perm, w_bits, Wq, ldwq, s_normal, s_outlier, bias, M, N, K, K_o, Y, ydt, ldy, workspace,
+                                       workspace_bytes, stream);
+        st != QARVD_OK)
+        return st;
+    return qarvd_qk_norm_rope(&q, heads_k ? &k : nullptr, ydt, M, D, norm, eps, rope, stream);
 }

@@ -45,6 +45,12 @@ struct GemmArgs {
     float out_scale;
     int32_t vec_out;   // every row of Y is whole, 16-byte aligned chunks; set by the entry points
     int32_t store_wt;  // (kernels on 64-byte stages) output stores write through the L2; set by the launchers
+    // fused endings: Y = R + gate[m / gate_rows] * act(y); either pointer may be null
+    const float *gate;
+    const void *R;     // of the output's type
+    int64_t ldg, ldr;
+    int32_t gate_rows;
+    int32_t K, K_o;    // as the caller gave them (the kernels go by n_off and kp)
 };
 
 // LDS image of an operand tile: row r at byte r*128, its eight 16-byte chunks XOR-swizzled by
@@ -100,6 +106,11 @@ qarvd_status launch_dma128_q8(const GemmArgs &g, hipStream_t st);
 // 128-byte-deep K stages (gemm_dma128.hip); GEN: two accumulator sets, any outlier width, any N and output alignment
 template <int BM, int BN, int WM, int WN, int NSTAGE, bool DUAL, bool GEN = false, bool W4 = false>
 qarvd_status launch_dma128(const GemmArgs &g, qarvd_dtype ydt, hipStream_t st);
+// fused endings (gemm_fused.hip): g.act, g.gate, g.R
+template <int BM, int BN, int WM, int WN, int NSTAGE, bool GEN, bool W4>
+qarvd_status launch_dma128_fused(const GemmArgs &g, qarvd_dtype ydt, hipStream_t st);
+template <bool W4>
+qarvd_status launch_staged_fused(const GemmArgs &g, qarvd_dtype ydt, hipStream_t st);
 template <int BM, int BN, int WM, int WN, int NSTAGE, bool DUAL>
 qarvd_status launch_mfma16(const GemmArgs &g, qarvd_dtype ydt, hipStream_t st);
 

@@ -5,11 +5,16 @@
 // loads 8 bytes where the INT8 build loads 16 and widens them to sixteen INT8 lanes holding 16 * code on the
 // way into LDS.  Both sums are then 16 times the INT8 ones and the weight scales are multiplied by 1/16 (exact
 // in fp32: a power of two), so every product and fma of the epilogue rounds the same value as the INT8 path.
-#include "gemm_common.h"
+// FUSED: activation, gate and residual (see GemmArgs) follow the dequantized sum; everything about them is decided at run time, in the
+// kernel that nothing but such strides reaches.
+#include "gemm_dma_common.h"
 
 namespace qarvd_gemm {
 
-template <int BM, int BN, int WM, int WN, bool DUAL, typename OutT, bool W4>
+__device__ __forceinline__ float widen_out(float r) { return r; }
+__device__ __forceinline__ float widen_out(uint16_t r) { return bf16_bits_to_f32(r); }
+
+template <int BM, int BN, int WM, int WN, bool DUAL, typename OutT, bool W4, bool FUSED>
 __global__ __launch_bounds__(TPB) void gemm_staged_kernel(GemmArgs g)
 {
     static_assert(WM * WN == 4, "four wavefronts");
@@ -152,6 +157,15 @@ __global__ __launch_bounds__(TPB) void gemm_staged_kernel(GemmArgs g)
                 v = fmaf((float)an, sn, v);
                 v = fmaf(v, sx_lds[ml], bs);
                 if (m < g.M && n < g.N) {
+                    if constexpr (FUSED) {
+                        if (g.act == QARVD_ACT_GELU_TANH) v = gelu_tanh(v);
+                        float r = 0.0f;
+                        if (g.R) r = widen_out(reinterpret_cast<const OutT *>(g.R)[(size_t)m * g.ldr + n]);
+                        if (g.gate || g.R) v = fmaf(g.gate ? g.gate[(size_t)((unsigned)m / (unsigned)g.gate_rows) * g.ldg + n] : 1.0f, v, r);
+                        if constexpr (sizeof(OutT) == 2) Y[(size_t)m * g.ldy + n] = (OutT)cvt_pk_bf16(v, 0.0f);     // (a residual may be NaN)
+                        else Y[(size_t)m * g.ldy + n] = v;
+                        continue;
+                    }
                     store_out<OutT>(Y + (size_t)m * g.ldy + n, v);
                     if (g.dbg_n) g.dbg_n[(size_t)m * g.N + n] = an >> (W4 ? 4 : 0);     // exact multiples of 16
                     if (g.dbg_o) g.dbg_o[(size_t)m * g.N + n] = ao >> (W4 ? 4 : 0);
@@ -161,8 +175,8 @@ __global__ __launch_bounds__(TPB) void gemm_staged_kernel(GemmArgs g)
     }
 }
 
-template <int BM, int BN, int WM, int WN, bool DUAL, bool W4>
-qarvd_status launch_staged(const GemmArgs &g0, qarvd_dtype ydt, hipStream_t st)
+template <int BM, int BN, int WM, int WN, bool DUAL, bool W4, bool FUSED>
+qarvd_status launch_staged_as(const GemmArgs &g0, qarvd_dtype ydt, hipStream_t st)
 {
     GemmArgs g = g0;
     g.tiles_m = (g.M + BM - 1) / BM;
@@ -170,12 +184,12 @@ qarvd_status launch_staged(const GemmArgs &g0, qarvd_dtype ydt, hipStream_t st)
     const size_t lds = 2 * (size_t)(BM + BN) * BK + BM * sizeof(float);
     const int grid = g.tiles_m * g.tiles_n;
     if (ydt == QARVD_BF16) {
-        auto k = gemm_staged_kernel<BM, BN, WM, WN, DUAL, uint16_t, W4>;
+        auto k = gemm_staged_kernel<BM, BN, WM, WN, DUAL, uint16_t, W4, FUSED>;
         static unsigned long long raised = 0;
         if (qarvd_status s_a = qarvd_raise_lds_limit_once(k, (int)lds, raised); s_a != QARVD_OK) return s_a;
         hipLaunchKernelGGL(k, dim3(grid), dim3(TPB), lds, st, g);
     } else {
-        auto k = gemm_staged_kernel<BM, BN, WM, WN, DUAL, float, W4>;
+        auto k = gemm_staged_kernel<BM, BN, WM, WN, DUAL, float, W4, FUSED>;
         static unsigned long long raised = 0;
         if (qarvd_status s_a = qarvd_raise_lds_limit_once(k, (int)lds, raised); s_a != QARVD_OK) return s_a;
         hipLaunchKernelGGL(k, dim3(grid), dim3(TPB), lds, st, g);
@@ -183,7 +197,20 @@ qarvd_status launch_staged(const GemmArgs &g0, qarvd_dtype ydt, hipStream_t st)
     return qarvd_launch_status();
 }
 
+template <int BM, int BN, int WM, int WN, bool DUAL, bool W4>
+qarvd_status launch_staged(const GemmArgs &g, qarvd_dtype ydt, hipStream_t st)
+{
+    return launch_staged_as<BM, BN, WM, WN, DUAL, W4, false>(g, ydt, st);
+}
 
+template <bool W4>
+qarvd_status launch_staged_fused(const GemmArgs &g, qarvd_dtype ydt, hipStream_t st)
+{
+    return launch_staged_as<128, 128, 2, 2, true, W4, true>(g, ydt, st);
+}
+
+template qarvd_status launch_staged_fused<false>(const GemmArgs &, qarvd_dtype, hipStream_t);
+template qarvd_status launch_staged_fused<true>(const GemmArgs &, qarvd_dtype, hipStream_t);
 template qarvd_status launch_staged<256, 128, 2, 2, true, false>(const GemmArgs &, qarvd_dtype, hipStream_t);
 template qarvd_status launch_staged<128, 128, 2, 2, true, false>(const GemmArgs &, qarvd_dtype, hipStream_t);
 template qarvd_status launch_staged<256, 128, 2, 2, false, false>(const GemmArgs &, qarvd_dtype, hipStream_t);
