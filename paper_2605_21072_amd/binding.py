@@ -147,6 +147,8 @@ def _load_host(lib):
     host.init([C.cast(f, C.c_void_p).value for f in (
         lib.qarvd_linear, lib.qarvd_linear_workspace, lib.qarvd_packed_ld, lib.qarvd_quant_act, lib.qarvd_quant_act_static,
         lib.qarvd_w8a8_dual_gemm_variant, lib.qarvd_w4a8_dual_gemm, lib.qarvd_w8a8_dual_gemm_q8)])
+    host.init_block([C.cast(f, C.c_void_p).value for f in (lib.qarvd_dual_gemm_fused, lib.qarvd_linear_fused, lib.qarvd_qk_norm_rope,
+                                                           lib.qarvd_linear_qkv)])
     _host = host
     return host
 
@@ -511,7 +513,7 @@ def _ending(M: int, N: int, act: int, gate, gate_rows, residual, dtype) -> Optio
             if groups == 0 or M % groups:
                 raise ValueError("%d tokens in %d groups: give gate_rows" % (M, groups))
             gate_rows = M // groups
-        if gate_rows < 1 or groups * gate_rows < M:
+        if gate_rows < 1 or groups < 1 or groups * gate_rows < M:
             raise ValueError("%d groups of %d tokens do not cover %d" % (groups, gate_rows, M))
         e.gate, e.gate_rows, e.ldg = gate.data_ptr(), min(gate_rows, M), gate.stride(0) if gate.dim() == 2 else N
     elif gate_rows is not None:
@@ -545,9 +547,18 @@ def w8a8_dual_gemm_fused(Xq: torch.Tensor, s_x: torch.Tensor, w: DualScaleWeight
     """qarvd_dual_gemm_fused: Y = residual + gate * act(dual GEMM + bias), INT8 or INT4 weights.  gate f32 [N], or [groups, N] for groups of
     gate_rows tokens (M / groups unless given); residual [M, N] of Y's type; Y may be the residual."""
     lib = load_library()
+    if host := _native(lib, stream):
+        st, Y = host.gemm_fused(Xq, s_x, w.bits, w.Wq, w.s_normal, w.s_outlier, bias, M, w.N, w.K, w.K_o, int(act), gate, residual, gate_rows, out_dtype if Y is None else None, Y,
+                                variant, _stream(None), torch._C._cuda_getDevice())
+        _check(st, "qarvd_dual_gemm_fused")
+        return Y
     dtype = out_dtype if Y is None else Y.dtype
     e = _ending(M, w.N, act, gate, gate_rows, residual, dtype)
-    _on_call_device(stream, Xq, s_x, w.Wq, gate, residual, Y)
+    if dtype not in _DTYPES:
+        raise TypeError("expected float32 or bfloat16, got %s" % dtype)
+    _on_call_device(stream, Xq, s_x, w.Wq, bias, gate, residual, Y)
+    if Xq.dim() != 2 or Xq.shape[0] < M:
+        raise ValueError("Xq has fewer than M rows")
     Y = _out(Y, M, w.N, dtype, Xq.device, stream)
     st = lib.qarvd_dual_gemm_fused(_ptr(Xq), Xq.stride(0), _ptr(s_x), w.bits, _ptr(w.Wq), w.Wq.stride(0), _ptr(w.s_normal), _ptr(w.s_outlier),
                                    _ptr(bias), C.byref(e), M, w.N, w.K, w.K_o, _ptr(Y), _dt(Y), _ld(Y), variant, _stream(stream))
@@ -560,13 +571,20 @@ def w8a8_linear_fused(X: torch.Tensor, w: DualScaleWeight, bias: Optional[torch.
                       Y: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """qarvd_linear_fused: quant_act followed by w8a8_dual_gemm_fused in one call."""
     lib = load_library()
+    if host := _native(lib, stream):
+        st, Y = host.linear_fused(X, w.perm, w.bits, w.Wq, w.s_normal, w.s_outlier, bias, w.N, w.K, w.K_o, int(act), gate, residual, gate_rows, out_dtype if Y is None else None, Y,
+                                  _stream(None), torch._C._cuda_getDevice())
+        _check(st, "qarvd_linear_fused")
+        return Y
     _dev2d(X, "X")
     M, K = X.shape
     if K != w.K:
         raise ValueError("X has %d channels, the layer %d" % (K, w.K))
     dtype = out_dtype if Y is None else Y.dtype
     e = _ending(M, w.N, act, gate, gate_rows, residual, dtype)
-    _on_call_device(stream, X, w.Wq, gate, residual, Y)
+    if dtype not in _DTYPES:
+        raise TypeError("expected float32 or bfloat16, got %s" % dtype)
+    _on_call_device(stream, X, w.Wq, bias, gate, residual, Y)
     need = lib.qarvd_linear_workspace(M, K, w.K_o)
     ws = _empty(need, torch.uint8, X.device, stream, scratch=True)
     Y = _out(Y, M, w.N, dtype, X.device, stream)
@@ -638,6 +656,12 @@ def qk_norm_rope(Q: torch.Tensor, K: Optional[torch.Tensor], norm: int = NORM_HE
     """qarvd_qk_norm_rope: RMS norm of each head (or a token's whole row) and rotation by `pos` int32 [M, axes].  Q [M, heads, D], K [M, heads_k, D] or
     None, f32 / bf16, any token and head strides.  Returns the outputs: out_q, out_k (Q and K themselves for in place) or new dense tensors."""
     lib = load_library()
+    if host := _native(lib, stream):
+        axes, freq, inter = (rope.axis_dims, rope.freq, rope.interleaved) if rope is not None else (None, None, False)
+        st, out_q, out_k = host.heads(Q, K, int(norm), weight_q, weight_k, eps, pos, axes, freq, bool(inter), out_q, out_k, _stream(None),
+                                      torch._C._cuda_getDevice())
+        _check(st, "qarvd_qk_norm_rope")
+        return out_q, out_k
     _check_heads(Q, "Q")
     M, hq, D = Q.shape
     _norm_weight(weight_q, norm, hq, D, "weight_q")
@@ -670,6 +694,12 @@ def w8a8_linear_qkv(X: torch.Tensor, w: DualScaleWeight, bias: Optional[torch.Te
     """qarvd_linear_qkv: the fused q / k / v projection with its queries and keys normed and rotated.  Returns Y [M, N], columns
     [heads_q * head_dim | heads_k * head_dim | values]."""
     lib = load_library()
+    if host := _native(lib, stream):
+        axes, freq, inter = (rope.axis_dims, rope.freq, rope.interleaved) if rope is not None else (None, None, False)
+        st, Y = host.linear_qkv(X, w.perm, w.bits, w.Wq, w.s_normal, w.s_outlier, bias, w.N, w.K, w.K_o, heads_q, heads_k, head_dim, int(norm), weight_q, weight_k, eps,
+                                pos, axes, freq, bool(inter), out_dtype, _stream(None), torch._C._cuda_getDevice())
+        _check(st, "qarvd_linear_qkv")
+        return Y
     _dev2d(X, "X")
     M, K = X.shape
     if K != w.K:
@@ -677,7 +707,7 @@ def w8a8_linear_qkv(X: torch.Tensor, w: DualScaleWeight, bias: Optional[torch.Te
     _norm_weight(weight_q, norm, heads_q, head_dim, "weight_q")
     _norm_weight(weight_k, norm, heads_k, head_dim, "weight_k")
     r = _rope(rope, pos, M)
-    _on_call_device(stream, X, w.Wq, weight_q, weight_k, pos, rope and rope.freq)
+    _on_call_device(stream, X, w.Wq, bias, weight_q, weight_k, pos, rope and rope.freq)
     need = lib.qarvd_linear_workspace(M, K, w.K_o)
     ws = _empty(need, torch.uint8, X.device, stream, scratch=True)
     Y = _empty((M, w.N), out_dtype, X.device, stream)

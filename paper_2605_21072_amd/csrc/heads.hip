@@ -1,6 +1,8 @@
 // Norm of queries and keys and their rotation by position (time, height, width), one pass over both.
 //
 //     r = 1 / sqrt(mean(x^2) + eps);   x <- x r w;   (a, b) <- (a cos t - b sin t, a sin t + b cos t),   t = pos[axis(i)] freq[i]
+#include <type_traits>
+
 #include "qarvd_common.h"
 
 namespace {
@@ -114,8 +116,332 @@ __global__ __launch_bounds__(TPB) void heads_any_kernel(HeadArgs a)
     }
 }
 
+// Rows in registers.  A wave has a token and CH vectors of its queries or keys; a vector is 64 lanes of 8 channels, lph (a power of two)
+// to a head, whole heads side by side.  All loads go out first, then lane i works out the angle of pair i, once for the
+// token instead of once in every lane that needs it, and the wave reads them back from LDS in the order of its channels: a lane's four pairs
+// are the same in every vector, so they stay in registers, like a head's weights.
+//   interleaved  the lane's channels are 8 j .. 8 j + 7, its pairs 4 j .. 4 j + 3
+//   HALF         channels 4 j .. and R/2 + 4 j .., the same pairs; lanes behind the rotary channels have 8 neighbours again
+// WHOLE: every lane's pieces are whole and 16-byte aligned (HALF bf16: 8).  Otherwise they are loaded from any address, and the last lane of a
+// head (HALF: also of its rotary channels) takes what there is one by one.
+struct FastArgs {
+    HeadArgs h;
+    int32_t lph_log, hpv_log;      // lanes to a head, heads to a vector (log2)
+    int32_t rotary_lanes;          // (HALF) lanes of a head that hold pairs
+    int32_t nv[2], parts_q;        // vectors of a token's queries and keys; how many waves share the queries
+    int32_t write_through;         // how the outputs leave (see stores_through)
+    float inv_n[2];                // 1 / (channels under a norm)
+};
+typedef float v4 __attribute__((ext_vector_type(4)));
+typedef float v4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+
+// Four neighbouring channels as they lie in memory, and the same at any element's address (one instruction whatever the alignment).
+template <typename T> struct Four;
+template <> struct Four<float> {
+    typedef v4 raw;
+    typedef v4_any raw_any;
+    static __device__ __forceinline__ raw of(const float (&e)[4]) { return v4{e[0], e[1], e[2], e[3]}; }
+    static __device__ __forceinline__ float get(raw r, int k) { return r[k]; }
+    static __device__ __forceinline__ raw pack(const float *f) { return v4{f[0], f[1], f[2], f[3]}; }
+};
+template <> struct Four<uint16_t> {
+    typedef u2 raw;
+    typedef uint32_t raw_any __attribute__((ext_vector_type(2), aligned(2)));
+    static __device__ __forceinline__ raw of(const uint16_t (&e)[4]) { return u2{e[0] | ((uint32_t)e[1] << 16), e[2] | ((uint32_t)e[3] << 16)}; }
+    static __device__ __forceinline__ float get(raw r, int k) { return __uint_as_float(k & 1 ? r[k >> 1] & 0xFFFF0000u : r[k >> 1] << 16); }
+    static __device__ __forceinline__ uint32_t pack2(float x, float y)
+    {
+        typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+        typedef float v2f __attribute__((ext_vector_type(2)));
+        const v2f f = {x, y};
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector(f, v2bf));
+    }
+    static __device__ __forceinline__ raw pack(const float *f) { return u2{pack2(f[0], f[1]), pack2(f[2], f[3])}; }
+};
+// The first n of four elements at p, zeros behind.
+template <typename T> __device__ __forceinline__ typename Four<T>::raw load_some(const T *p, int n)
+{
+    if (n == 4) return *reinterpret_cast<const typename Four<T>::raw_any *>(p);
+    T e[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) e[k] = k < n ? p[k] : (T)0;
+    return Four<T>::of(e);
+}
+template <typename T> __device__ __forceinline__ void store_some(T *p, int n, typename Four<T>::raw r)
+{
+    if (n == 4) {
+        *reinterpret_cast<typename Four<T>::raw_any *>(p) = r;
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+        if (k < n) {
+            if constexpr (sizeof(T) == 4) p[k] = r[k];
+            else p[k] = (T)(r[k >> 1] >> (16 * (k & 1)));
+        }
+}
+
+// A piece to out + off (bytes), written through the L2 (sc0 sc1); out is the same in all lanes.
+template <typename P> __device__ __forceinline__ void store_through(void *out, int off, P piece)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(out, 0, 0x7fffffff, 0x00020000);
+    if constexpr (sizeof(P) == 16) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, piece), r, off, 0, 17);
+    else __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u2, piece), r, off, 0, 17);
+#else
+    (void)out; (void)off; (void)piece;
+#endif
+}
+
+// Sums over groups of 2^log neighbouring lanes, in every lane of the group, of several values at once (`log` is uniform).
+template <int CH> __device__ __forceinline__ void group_sum(float (&v)[CH], int log)
+{
+    auto all = [&](auto move) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) v[c] += __int_as_float(move(__float_as_int(v[c])));
+    };
+    if (log > 0) all([](int x) { return __builtin_amdgcn_update_dpp(0, x, 0xB1, 0xF, 0xF, false); });       // quad_perm 1,0,3,2
+    if (log > 1) all([](int x) { return __builtin_amdgcn_update_dpp(0, x, 0x4E, 0xF, 0xF, false); });       // quad_perm 2,3,0,1
+    if (log > 2) all([](int x) { return __builtin_amdgcn_update_dpp(0, x, 0x141, 0xF, 0xF, false); });      // mirrored in 8: the other four
+    if (log > 3) all([](int x) { return __builtin_amdgcn_update_dpp(0, x, 0x140, 0xF, 0xF, false); });      // mirrored in 16: the other eight
+    if (log > 4) all([](int x) { return __shfl_xor(x, 16, 64); });
+    if (log > 5) all([](int x) { return __shfl_xor(x, 32, 64); });
+}
+
+template <typename T, int CH, bool HALF, int NORM, bool WHOLE>
+__global__ __launch_bounds__(TPB) void heads_kernel(FastArgs f)
+{
+    typedef typename Four<T>::raw raw;
+    constexpr bool WIDE = WHOLE && !HALF && sizeof(T) == 2;         // the eight channels are one 16-byte piece
+    __shared__ __align__(16) float turns[TPB / 64][MAX_D];
+    const HeadArgs &a = f.h;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int m = blockIdx.x * (TPB / 64) + wave;
+    if (m >= a.M) return;
+    const bool keys = (int)blockIdx.y >= f.parts_q;
+    const Tensor &t = a.t[keys];
+    const int first = ((int)blockIdx.y - (keys ? f.parts_q : 0)) * CH;     // vector
+    const int j = lane & ((1 << f.lph_log) - 1), sub = lane >> f.lph_log;
+    const bool rotary = 4 * j < a.pairs;
+    const int rest = HALF ? 2 * a.pairs + 8 * (j - f.rotary_lanes) : 8 * j;       // first channel of a lane with eight neighbours
+    const int c0 = HALF && rotary ? 4 * j : rest, apart = HALF && rotary ? a.pairs : 4;
+    auto some = [](int left) { return min(max(left, 0), 4); };
+    const int n0 = HALF && rotary ? some(a.pairs - 4 * j) : some(a.D - rest), n1 = HALF && rotary ? n0 : some(a.D - rest - 4);
+    const bool inside = n0 > 0;
+
+    const T *x = reinterpret_cast<const T *>(t.x) + (size_t)m * t.ld + c0;
+    raw v[CH][2];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        v[c][0] = v[c][1] = raw{};
+        const int head = ((first + c) << f.hpv_log) + sub;
+        if (inside && head < t.heads) {
+            const T *p = x + (size_t)head * t.hs;
+            if constexpr (WIDE) {
+                const u4 r = *reinterpret_cast<const u4 *>(p);
+                v[c][0] = raw{r.x, r.y};
+                v[c][1] = raw{r.z, r.w};
+            } else if constexpr (WHOLE) {
+                v[c][0] = *reinterpret_cast<const raw *>(p);
+                v[c][1] = *reinterpret_cast<const raw *>(p + apart);
+            } else {
+                v[c][0] = load_some<T>(p, n0);
+                v[c][1] = load_some<T>(p + apart, n1);
+            }
+        }
+    }
+
+    float w[8];
+    auto load_weights = [&](const float *p) {
+        const v4 w0 = WHOLE ? (v4) * reinterpret_cast<const v4_any *>(p) : load_some<float>(p, n0);
+        const v4 w1 = WHOLE ? (v4) * reinterpret_cast<const v4_any *>(p + apart) : load_some<float>(p + apart, n1);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) { w[k] = w0[k]; w[4 + k] = w1[k]; }
+    };
+#pragma unroll
+    for (int k = 0; k < 8; ++k) w[k] = 1.0f;
+    if (NORM == QARVD_NORM_HEAD && t.w && inside) load_weights(t.w + c0);
+
+    float co[4], si[4];
+    if (a.pairs) {
+        float *const mine = turns[wave];
+        const int32_t *pos = a.pos + (size_t)m * a.ldpos;
+        for (int i = lane; i < a.pairs; i += 64) {
+            const float2 cs = cos_sin(pos[axis_of(a, i)], a.freq[i]);
+            mine[i] = cs.x;
+            mine[MAX_D / 2 + i] = cs.y;
+        }
+        __builtin_amdgcn_wave_barrier();                   // (one wave's LDS accesses complete in order)
+        const v4 c4 = *reinterpret_cast<const v4 *>(mine + 4 * j), s4 = *reinterpret_cast<const v4 *>(mine + MAX_D / 2 + 4 * j);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) { co[k] = c4[k]; si[k] = s4[k]; }
+    }
+
+    float scale[CH];
+    if constexpr (NORM != QARVD_NORM_NONE) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            scale[c] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float e = Four<T>::get(v[c][k >> 2], k & 3);
+                scale[c] = fmaf(e, e, scale[c]);
+            }
+        }
+        if constexpr (NORM == QARVD_NORM_ROW) {
+#pragma unroll
+            for (int c = 1; c < CH; ++c) scale[0] += scale[c];
+            float sum[1] = {scale[0]};
+            group_sum<1>(sum, 6);
+#pragma unroll
+            for (int c = 0; c < CH; ++c) scale[c] = sum[0];
+        } else {
+            group_sum<CH>(scale, f.lph_log);
+        }
+#pragma unroll
+        for (int c = 0; c < CH; ++c) scale[c] = rsqrtf(fmaf(scale[c], f.inv_n[keys], a.eps));
+    }
+
+    T *const out = reinterpret_cast<T *>(t.out) + (size_t)m * t.ld_out;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int head = ((first + c) << f.hpv_log) + sub;
+        if (!inside || head >= t.heads) continue;
+        float e[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) e[k] = Four<T>::get(v[c][k >> 2], k & 3);
+        if constexpr (NORM != QARVD_NORM_NONE) {
+            if (NORM == QARVD_NORM_ROW && t.w) load_weights(t.w + (size_t)head * a.D + c0);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) e[k] = e[k] * scale[c] * w[k];
+        }
+        if (a.pairs) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int p = HALF ? k : 2 * k, q = HALF ? 4 + k : 2 * k + 1;
+                const float u = e[p], z = e[q];
+                const float up = fmaf(u, co[k], -(z * si[k])), zp = fmaf(u, si[k], z * co[k]);
+                const bool turn = 4 * j + k < a.pairs;     // (selected, not multiplied by 1 and 0: the rest may be infinite)
+                e[p] = turn ? up : u;
+                e[q] = turn ? zp : z;
+            }
+        }
+        const int64_t at = (int64_t)head * t.hs_out + c0;      // from the token's first element
+        const raw lo = Four<T>::pack(e), hi = Four<T>::pack(e + 4);
+        if constexpr (!WHOLE) {
+            store_some<T>(out + at, n0, lo);
+            store_some<T>(out + at + apart, n1, hi);
+        } else {
+            auto put = [&](int k, auto piece) {
+                if (f.write_through) store_through(out, (int)(at + k) * (int)sizeof(T), piece);
+                else __builtin_nontemporal_store(piece, reinterpret_cast<decltype(piece) *>(out + at + k));
+            };
+            if constexpr (WIDE) {
+                put(0, u4{lo.x, lo.y, hi.x, hi.y});
+            } else {
+                put(0, lo);
+                put(apart, hi);
+            }
+        }
+    }
+}
+
+int ceil_log2(int n)
+{
+    int l = 0;
+    while ((1 << l) < n) ++l;
+    return l;
+}
+
+template <typename T, bool HALF, int NORM, bool WHOLE> bool launch_fast(const FastArgs &f, int ch, int parts, hipStream_t st)
+{
+    const dim3 grid((f.h.M + TPB / 64 - 1) / (TPB / 64), parts);
+    auto go = [&](auto n) {
+        hipLaunchKernelGGL((heads_kernel<T, decltype(n)::value, HALF, NORM, WHOLE>), grid, dim3(TPB), 0, st, f);
+        return true;
+    };
+    switch (ch) {
+    case 1: return go(std::integral_constant<int, 1>{});
+    case 2: return go(std::integral_constant<int, 2>{});
+    case 3: return go(std::integral_constant<int, 3>{});
+    case 4: return go(std::integral_constant<int, 4>{});
+    case 5: return go(std::integral_constant<int, 5>{});
+    case 6: return go(std::integral_constant<int, 6>{});
+    case 8: return go(std::integral_constant<int, 8>{});
+    case 10: return go(std::integral_constant<int, 10>{});
+    case 16: return go(std::integral_constant<int, 16>{});
+    }
+    return false;
+}
+// The vectors a wave gets at least `ch` of, rounded up to a kernel that is built.
+int built(int ch) { return ch <= 6 ? ch : ch <= 8 ? 8 : ch <= 10 ? 10 : ch <= 16 ? 16 : 0; }
+
+// Vectors to a wave: as few as leave every SIMD some waves, since a wave works out its token's angles whatever it has, and at most four.  us for 1, 2, 3, 4
+// and 6: 4680 x 24 heads of 128 bf16 14.3, 13.9, 12.3, 12.3, 12.3; 1560 x 24 5.97, 5.60, 5.60, 5.63, 5.66; 520 x 80 fp32 8.98, 8.77, 8.73, 9.05, 9.47;
+// 64 x 24 2.71, 2.87, 3.10, 3.12, 3.12; one token 2.41, 2.55, 2.82, 2.81, 2.81.
+constexpr int64_t WAVES = 4096;
+
+// Stores that write through the L2, or such with the non-temporal hint.  Nothing is left to write back when the kernel ends with either; written
+// through, the last-level cache (256 MB) still has the outputs for attention.  us plain, through, non-temporal, and the same with a copy of the
+// outputs behind it:  4680 x 24 heads of 128 bf16 (58 MB in and out) 12.3, 11.1, 11.1 | 24.0, 22.3, 25.7;  1560 x 24 (19 MB) 5.9, 4.8, 4.8 | 13.9, 13.0, 14.1;
+// 32760 x 24 (403 MB), more than that cache holds, 79.8, 79.8, 73.8 | 157.6, 157.3, 156.4.
+int32_t stores_through(const HeadArgs &a, size_t esz)
+{
+    size_t bytes = 0;
+    for (const Tensor &t : a.t) {
+        bytes += 2 * (size_t)a.M * t.heads * a.D * esz;
+        if (t.heads > 1 && (t.heads - 1) * t.hs_out * (int64_t)esz > 0x7f000000) return 0;      // (32-bit offsets from the token)
+    }
+    return bytes <= ((size_t)256 << 20) ? 1 : 0;
+}
+
+bool pieces_ok(const Tensor &t, int32_t M, size_t esz)
+{
+    const int64_t per = 16 / (int64_t)esz;
+    return t.heads == 0 || (qarvd_aligned16(t.x) && qarvd_aligned16(t.out) && (M == 1 || (t.ld % per == 0 && t.ld_out % per == 0)) &&
+                            (t.heads == 1 || (t.hs % per == 0 && t.hs_out % per == 0)));
+}
+
 template <typename T> qarvd_status launch(const HeadArgs &a, hipStream_t st)
 {
+    const bool half = a.pairs > 0 && !a.interleaved;
+    const bool whole = a.D % 8 == 0 && !(half && a.pairs % 4) && pieces_ok(a.t[0], a.M, sizeof(T)) && pieces_ok(a.t[1], a.M, sizeof(T));
+    FastArgs f;
+    f.h = a;
+    f.rotary_lanes = half ? (a.pairs + 3) / 4 : 0;
+    const int lanes = f.rotary_lanes + ((half ? a.D - 2 * a.pairs : a.D) + 7) / 8;
+    if (lanes <= 64) {
+        f.lph_log = ceil_log2(lanes);
+        f.hpv_log = 6 - f.lph_log;
+        for (int i = 0; i < 2; ++i) {
+            f.nv[i] = (a.t[i].heads + (1 << f.hpv_log) - 1) >> f.hpv_log;
+            f.inv_n[i] = 1.0f / (float)(a.norm == QARVD_NORM_ROW ? (int64_t)a.t[i].heads * a.D : (int64_t)a.D);
+        }
+        const int most = f.nv[0] > f.nv[1] ? f.nv[0] : f.nv[1];
+        int ch = most;                       // a row's norm: one wave for all of it
+        if (a.norm != QARVD_NORM_ROW) {
+            const int64_t vectors = (int64_t)a.M * (f.nv[0] + f.nv[1]);
+            const int want = vectors >= 4 * WAVES ? 4 : vectors >= 2 * WAVES ? (int)(vectors / WAVES) : 1;
+            const int waves = (most + want - 1) / want;
+            ch = (most + waves - 1) / waves;       // evenly
+        }
+        f.write_through = stores_through(a, sizeof(T));
+        ch = built(ch);
+        if (ch > 0) {
+            f.parts_q = (f.nv[0] + ch - 1) / ch;
+            const int parts = f.parts_q + (f.nv[1] + ch - 1) / ch;
+            auto as = [&](auto norm) {
+                constexpr int N = decltype(norm)::value;
+                if (whole) return half ? launch_fast<T, true, N, true>(f, ch, parts, st) : launch_fast<T, false, N, true>(f, ch, parts, st);
+                return half ? launch_fast<T, true, N, false>(f, ch, parts, st) : launch_fast<T, false, N, false>(f, ch, parts, st);
+            };
+            const bool ran = a.norm == QARVD_NORM_NONE ? as(std::integral_constant<int, QARVD_NORM_NONE>{})
+                             : a.norm == QARVD_NORM_HEAD ? as(std::integral_constant<int, QARVD_NORM_HEAD>{}) : as(std::integral_constant<int, QARVD_NORM_ROW>{});
+            if (ran) return qarvd_launch_status();
+        }
+    }
     hipLaunchKernelGGL((heads_any_kernel<T>), dim3(a.M, a.t[1].heads > 0 ? 2 : 1), dim3(TPB), 0, st, a);
     return qarvd_launch_status();
 }

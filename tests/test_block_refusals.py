@@ -84,68 +84,77 @@ def test_heads(lib):
 
 
 class Fake(torch.Tensor):
-    """A host tensor that says it is on the device, for the binding's own checks."""
+    """A host tensor that says it is on the device, for the Python path's own checks."""
     is_cuda = True
 
 
-def fake(t):
-    return t.as_subclass(Fake)
-
-
-@pytest.fixture
-def host(lib, monkeypatch):
-    """The binding's checks run as on a GPU; a call that passes them fails the test."""
-    monkeypatch.setattr(binding, "_on_call_device", lambda *a: None)
-    monkeypatch.setattr(binding, "_stream", lambda s: 0)
-
-
-def test_binding_checks_the_ending(host):
+def bad_endings(put):
     M, N, K = 4, 8, 128
-    X = fake(torch.zeros(M, K))
-    w = q.DualScaleWeight(torch.zeros((N, 256), dtype=torch.int8), torch.ones(N), torch.ones(N), None, 0, N, K)
-    f, b = torch.zeros(M, N), torch.zeros(M, N, dtype=torch.bfloat16)
-    for bad, err in ((dict(gate=torch.zeros(N, dtype=torch.bfloat16)), TypeError), (dict(gate=torch.zeros(N + 1)), ValueError),
-                     (dict(gate=torch.zeros(3, N)), ValueError), (dict(gate=torch.zeros(2, N), gate_rows=1), ValueError),
-                     (dict(gate=torch.zeros(2, N), gate_rows=0), ValueError), (dict(gate=torch.zeros(0, N)), ValueError),
-                     (dict(gate=torch.zeros(N, 4).t()[:, ::1][:1].expand(1, N)), ValueError), (dict(gate_rows=2), ValueError),
-                     (dict(gate=torch.zeros(2, 2, N)), ValueError),
+    X, Xq = put(torch.zeros(M, K)), put(torch.zeros((M, 256), dtype=torch.int8))
+    w = q.DualScaleWeight(put(torch.zeros((N, 256), dtype=torch.int8)), put(torch.ones(N)), put(torch.ones(N)), None, 0, N, K)
+    f, b, z = put(torch.zeros(M, N)), put(torch.zeros(M, N, dtype=torch.bfloat16)), lambda *s, **k: put(torch.zeros(*s, **k))
+    for bad, err in ((dict(gate=z(N, dtype=torch.bfloat16)), TypeError), (dict(gate=z(N + 1)), ValueError),
+                     (dict(gate=z(3, N)), ValueError), (dict(gate=z(2, N), gate_rows=1), ValueError),
+                     (dict(gate=z(2, N), gate_rows=0), ValueError), (dict(gate=z(2, N), gate_rows=-4), ValueError), (dict(gate=z(0, N)), ValueError),
+                     (dict(gate=z(0, N), gate_rows=4), ValueError), (dict(gate=z(N, 4).t()[:1]), ValueError), (dict(gate_rows=2), ValueError),
+                     (dict(gate=z(2, 2, N)), ValueError), (dict(act=5), q.QarvdError),
                      (dict(residual=f), TypeError), (dict(residual=b[:3]), ValueError), (dict(residual=b[:, :7]), ValueError),
-                     (dict(residual=b.t().contiguous().t()), ValueError), (dict(residual=b, out_dtype=torch.float32), TypeError),
-                     (dict(Y=b[:2]), ValueError), (dict(Y=b.t().contiguous().t()), ValueError), (dict(out_dtype=torch.float16), TypeError)):
-        with pytest.raises(err):
-            q.w8a8_linear_fused(X, w, None, **bad)
-        with pytest.raises(err):
-            q.w8a8_dual_gemm_fused(torch.zeros((M, 256), dtype=torch.int8), torch.ones(M), w, None, M, **bad)
-    with pytest.raises(ValueError):
-        q.w8a8_linear_fused(fake(torch.zeros(M, K - 1)), w, None)
-    with pytest.raises(ValueError):
-        q.w8a8_linear_fused(torch.zeros(M, K), w, None)              # not on the device
+                     (dict(residual=z(N, M, dtype=torch.bfloat16).t()), ValueError), (dict(residual=b, out_dtype=torch.float32), TypeError),
+                     (dict(Y=b[:2]), ValueError), (dict(Y=z(N, M).t()), ValueError), (dict(out_dtype=torch.float16), TypeError)):
+        yield lambda s, bad=bad: q.w8a8_linear_fused(X, w, None, stream=s, **bad), err
+        yield lambda s, bad=bad: q.w8a8_dual_gemm_fused(Xq, put(torch.ones(M)), w, None, M, stream=s, **bad), err
+    yield lambda s: q.w8a8_linear_fused(put(torch.zeros(M, K - 1)), w, None, stream=s), ValueError
+    yield lambda s: q.w8a8_linear_fused(torch.zeros(M, K), w, None, stream=s), ValueError              # not on the device
+    yield lambda s: q.w8a8_dual_gemm_fused(Xq, put(torch.ones(9)), w, None, M + 1, stream=s), ValueError
 
 
-def test_binding_checks_the_heads(host):
+def bad_heads(put):
     M, H, D = 4, 2, 64
-    Q, K = fake(torch.zeros(M, H, D)), fake(torch.zeros(M, 1, D))
-    pos, rope = torch.zeros((M, 2), dtype=torch.int32), q.Rope((32, 32), torch.zeros(32, dtype=torch.float64))
-    for args, err in ((dict(Q=torch.zeros(M, H, D)), ValueError), (dict(Q=Q[0]), ValueError), (dict(Q=fake(torch.zeros(M, D, H)).transpose(1, 2)), ValueError),
-                      (dict(K=fake(torch.zeros(M + 1, 1, D))), ValueError), (dict(K=fake(torch.zeros(M, 1, D - 2))), ValueError),
-                      (dict(K=K.bfloat16()), ValueError), (dict(K=None, out_k=Q), ValueError), (dict(K=None, weight_k=torch.ones(D)), ValueError),
-                      (dict(weight_q=torch.ones(D - 1)), ValueError), (dict(weight_q=torch.ones(2 * D)), ValueError),
-                      (dict(weight_q=torch.ones(D), norm=q.NORM_ROW), ValueError), (dict(weight_q=torch.ones(D), norm=q.NORM_NONE), ValueError),
-                      (dict(weight_k=torch.ones(D, dtype=torch.float64)), TypeError), (dict(weight_q=torch.ones(2 * D)[::2]), ValueError),
+    z = lambda *s, **k: put(torch.zeros(*s, **k))       # noqa: E731
+    Q, K = z(M, H, D), z(M, 1, D)
+    pos, freq = z((M, 2), dtype=torch.int32), z(32, dtype=torch.float64)
+    rope = q.Rope((32, 32), freq)
+    for args, err in ((dict(Q=torch.zeros(M, H, D)), ValueError), (dict(Q=Q[0]), ValueError), (dict(Q=z(M, D, H).transpose(1, 2)), ValueError),
+                      (dict(K=z(M + 1, 1, D)), ValueError), (dict(K=z(M, 1, D - 2)), ValueError), (dict(K=K.bfloat16()), ValueError),
+                      (dict(Q=Q.half(), K=K.half()), TypeError),
+                      (dict(K=None, out_k=Q), ValueError), (dict(K=None, weight_k=z(D)), ValueError),
+                      (dict(weight_q=z(D - 1)), ValueError), (dict(weight_q=z(2 * D)), ValueError),
+                      (dict(weight_q=z(D), norm=q.NORM_ROW), ValueError), (dict(weight_q=z(D), norm=q.NORM_NONE), ValueError),
+                      (dict(weight_k=z(D, dtype=torch.float64)), TypeError), (dict(weight_q=z(2 * D)[::2]), ValueError),
                       (dict(out_q=K), ValueError), (dict(out_q=Q.bfloat16()), ValueError), (dict(out_q=torch.zeros(M, H, D)), ValueError),
+                      (dict(norm=3), q.QarvdError), (dict(eps=-1.0), q.QarvdError), (dict(Q=Q[:, :, :0], K=None), q.QarvdError),
+                      (dict(Q=Q.expand(M, H, D)[:, :1].expand(M, 2, D)), q.QarvdError),                 # heads on top of each other
                       (dict(pos=pos), ValueError), (dict(rope=rope), TypeError), (dict(rope=rope, pos=pos.long()), TypeError),
                       (dict(rope=rope, pos=pos[:3]), ValueError), (dict(rope=rope, pos=pos[:, :1]), ValueError),
-                      (dict(rope=q.Rope((64,), rope.freq), pos=pos), ValueError), (dict(rope=q.Rope((32, 32), rope.freq.float()), pos=pos), TypeError),
-                      (dict(rope=q.Rope((32, 30), rope.freq), pos=pos), ValueError), (dict(rope=q.Rope((), rope.freq), pos=pos), ValueError),
-                      (dict(rope=q.Rope((16, 16, 16, 16), rope.freq), pos=pos), ValueError)):
+                      (dict(rope=q.Rope((64,), freq), pos=pos), ValueError), (dict(rope=q.Rope((32, 32), freq.float()), pos=pos), TypeError),
+                      (dict(rope=q.Rope((32, 30), freq), pos=pos), ValueError), (dict(rope=q.Rope((), freq), pos=pos), ValueError),
+                      (dict(rope=q.Rope((65, -1), freq), pos=pos), q.QarvdError), (dict(rope=q.Rope((16, 16, 16, 16), freq), pos=pos), ValueError)):
+        yield lambda s, a={**dict(Q=Q, K=K), **args}: q.qk_norm_rope(stream=s, **a), err
+    w = q.DualScaleWeight(z((192, 256), dtype=torch.int8), put(torch.ones(192)), put(torch.ones(192)), None, 0, 192, 128)
+    X = z(M, 128)
+    for args, err in ((dict(heads_q=4), q.QarvdError), (dict(heads_q=0), q.QarvdError), (dict(weight_q=z(63)), ValueError), (dict(pos=pos), ValueError),
+                      (dict(norm=7), q.QarvdError), (dict(eps=-1.0), q.QarvdError), (dict(out_dtype=torch.float16), TypeError)):
+        yield lambda s, a={**dict(heads_q=2, heads_k=1, head_dim=64), **args}: q.w8a8_linear_qkv(X, w, None, stream=s, **a), err
+
+
+@pytest.mark.parametrize("calls", [bad_endings, bad_heads])
+def test_the_binding_refuses(lib, monkeypatch, calls):
+    monkeypatch.setattr(binding, "_native", lambda lib, stream: None)
+    monkeypatch.setattr(binding, "_on_call_device", lambda *a: None)
+    monkeypatch.setattr(binding, "_stream", lambda s: 0)
+    for call, err in calls(lambda t: t.as_subclass(Fake)):
         with pytest.raises(err):
-            q.qk_norm_rope(**{**dict(Q=Q, K=K), **args})
-    w = q.DualScaleWeight(torch.zeros((192, 256), dtype=torch.int8), torch.ones(192), torch.ones(192), None, 0, 192, 128)
-    X = fake(torch.zeros(M, 128))
-    for args, err in ((dict(heads_q=4), q.QarvdError), (dict(heads_q=0), q.QarvdError), (dict(weight_q=torch.ones(63)), ValueError),
-                      (dict(pos=pos), ValueError), (dict(norm=7), q.QarvdError), (dict(eps=-1.0), q.QarvdError)):
-        with pytest.raises(err):
-            q.w8a8_linear_qkv(X, w, None, **{**dict(heads_q=2, heads_k=1, head_dim=64), **args})
+            call(None)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("calls", [bad_endings, bad_heads])
+def test_both_marshallings_refuse_the_same(calls):
+    s = torch.cuda.Stream()
+    for call, err in calls(lambda t: t.cuda()):
+        for stream in (None, s):
+            with pytest.raises(err):
+                call(stream)
 
 
 def test_tensors_of_another_device_are_refused(lib, monkeypatch):
