@@ -11,7 +11,7 @@ from pathlib import Path
 PKG = Path(__file__).resolve().parent
 CSRC = PKG / "csrc"
 LIB = PKG / "libqarvd.so"
-SOURCES = ["quant_act.hip", "quantize_weight.hip", "gemm_api.hip", "gemm_staged.hip", "gemm_dma.hip", "gemm_dma128.hip", "gemm_mfma16.hip", "gemm_fused.hip", "gemm_fused_general.hip",
+SOURCES = ["quant_act.hip", "quantize_weight.hip", "gemm_api.hip", "gemm_staged.hip", "gemm_dma.hip", "gemm_dma128.hip", "gemm_mfma16.hip", "gemm_fused.hip", "gemm_fused_general.hip", "gemm_rows.hip",
            "heads.hip", "probe.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # QARVD_PROF=1 in the environment compiles the GEMM kernels with their per-wave tick counters

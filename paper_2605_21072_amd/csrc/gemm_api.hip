@@ -334,7 +334,7 @@ extern "C" qarvd_status qarvd_w8a8_dual_gemm_q8(const int8_t *Xq, int64_t ldxq, 
 namespace {
 struct FusedVariant {
     int BM, BN, bits;
-    int form;           // of the W4 variants: 0 aligned and an outlier block of at most 128 bytes, 1 strides up to 2^22, 2 anything
+    int form;           // 0: as the aligned tiles need it, 1: strides up to 2^22, 2: anything, 3: at most BM rows
     double c, a, b;     // cost model of pick_variant
     qarvd_status (*launch)(const GemmArgs &, qarvd_dtype, hipStream_t);
 };
@@ -356,6 +356,15 @@ const FusedVariant kFusedVariants[] = {
     {128, 128, 4, 1, 2.74, 3.47, 0.196, launch_dma128_fused<128, 128, 2, 4, 3, true, true>},
     {64, 64, 4, 1, 3.60, 1.00, 0.101, launch_dma128_fused<64, 64, 2, 2, 3, true, true>},
     {128, 128, 4, 2, 0, 0, 0, launch_staged_fused<true>},
+    {8, 8, 8, 3, 0, 0, 0, launch_rows_gemm<1, 1, 2, false>},
+    {16, 16, 8, 3, 0, 0, 0, launch_rows_gemm<1, 1, 1, false>},
+    {16, 32, 8, 3, 0, 0, 0, launch_rows_gemm<1, 2, 1, false>},
+    {32, 16, 8, 3, 0, 0, 0, launch_rows_gemm<2, 1, 1, false>},
+    {8, 8, 4, 3, 0, 0, 0, launch_rows_gemm<1, 1, 2, true>},
+    {16, 16, 4, 3, 0, 0, 0, launch_rows_gemm<1, 1, 1, true>},
+    {16, 32, 4, 3, 0, 0, 0, launch_rows_gemm<1, 2, 1, true>},
+    {32, 16, 4, 3, 0, 0, 0, launch_rows_gemm<2, 1, 1, true>},
+    {32, 32, 4, 3, 0, 0, 0, launch_rows_gemm<2, 2, 1, true>},
 };
 constexpr int kNumFusedVariants = sizeof(kFusedVariants) / sizeof(kFusedVariants[0]);
 
@@ -384,6 +393,21 @@ qarvd_status fill_ending(const qarvd_ending *e, qarvd_dtype ydt, GemmArgs *g)
     return QARVD_OK;
 }
 
+// Kernels for few rows (gemm_rows.hip): the narrowest whose workgroups all have a CU, up to sixteen rows also more of them than CUs where the weights
+// are INT4.  Wider outputs are the tiles': us at their limits, rows and best tile, INT8 1 x 1536 -> 8960 7.3 and 6.8, 16 x 1536 -> 8960 10.6 and
+// 6.8, 32 x 1536 -> 4608 8.3 and 7.0; INT4 16 x 4096 -> 13824 12.2 and 15.4, 32 x 4096 -> 4608 11.1 and 12.8, 32 x 4096 -> 8960 14 and 13.  0: none.
+int32_t pick_rows(int bits, const GemmArgs &g)
+{
+    const int cus = device_cus();
+    for (int i = 0; i < kNumFusedVariants; ++i) {
+        const FusedVariant &v = kFusedVariants[i];
+        if (v.form != 3 || v.bits != bits || g.M > v.BM || (v.BM == 32 && g.M <= 16)) continue;
+        const bool widest = v.BM == 16 && v.BN == 32;
+        if (g.N <= v.BN * cus || (widest && bits == 4)) return i + 1;
+    }
+    return 0;
+}
+
 qarvd_status launch_fused(int bits, int32_t variant, const GemmArgs &g, qarvd_dtype ydt, void *stream)
 {
     if (variant == 0) {
@@ -395,6 +419,9 @@ qarvd_status launch_fused(int bits, int32_t variant, const GemmArgs &g, qarvd_dt
             return qarvd_w8a8_dual_gemm(g.Xq, g.ldxq, g.s_x, g.Wq, g.ldwq, g.s_n, g.s_o, g.bias, g.M, g.N, g.K, g.K_o, g.Y, ydt, g.ldy, nullptr,
                                         nullptr, stream);
         }
+        variant = pick_rows(bits, g);
+    }
+    if (variant == 0) {
         const bool fast_ok = g.n_off <= 128 && g.vec_out;
         // (INT4: the any-width tiles stand beside the aligned ones, as for the plain GEMM)
         const int form = !short_rows_ok(g) ? 2 : fast_ok ? 0 : 1;
@@ -407,7 +434,8 @@ qarvd_status launch_fused(int bits, int32_t variant, const GemmArgs &g, qarvd_dt
         variant = cheapest(cand, n, g);
     }
     const FusedVariant &v = kFusedVariants[variant - 1];
-    if (v.bits != bits || (v.form == 0 && !(g.n_off <= 128 && g.vec_out)) || (v.form == 1 && !short_rows_ok(g))) return QARVD_ERR_UNSUPPORTED;
+    if (v.bits != bits || (v.form == 0 && !(g.n_off <= 128 && g.vec_out)) || (v.form == 1 && !short_rows_ok(g)) || (v.form == 3 && g.M > v.BM))
+        return QARVD_ERR_UNSUPPORTED;
     return v.launch(g, ydt, reinterpret_cast<hipStream_t>(stream));
 }
 }  // namespace
@@ -443,7 +471,7 @@ namespace {
 qarvd_status quantize_for_gemm(const void *X, qarvd_dtype xdt, int64_t ldx, const int32_t *perm, int32_t w_bits, const void *Wq, int64_t ldwq,
                                const float *s_normal, const float *s_outlier, const float *bias, const qarvd_ending *ending, int32_t M,
                                int32_t N, int32_t K, int32_t K_o, void *Y, qarvd_dtype ydt, int64_t ldy, void *workspace,
-                               size_t workspace_bytes, void *stream, GemmArgs *g)
+                               size_t workspace_bytes, void *stream, GemmArgs *g, bool *quantized = nullptr)
 {
     const size_t need = qarvd_linear_workspace(M, K, K_o);
     if (need == 0 || (w_bits != 8 && w_bits != 4)) return QARVD_ERR_INVALID_ARG;
@@ -456,6 +484,13 @@ qarvd_status quantize_for_gemm(const void *X, qarvd_dtype xdt, int64_t ldx, cons
         s_c != QARVD_OK)
         return s_c;
     if (qarvd_status s_e = fill_ending(ending, ydt, g); s_e != QARVD_OK) return s_e;
+    if (ending && rows_quant_fits(*g, device_cus())) {
+        *quantized = true;
+        const int32_t *p = K_o > 0 ? perm : nullptr;
+        if (qarvd_status st = qarvd_quant_act_check(X, xdt, M, K, ldx, p, K_o, Xq, ld, s_x); st != QARVD_OK) return st;
+        return w_bits == 4 ? launch_rows_quant<true>(*g, X, xdt, p, ydt, reinterpret_cast<hipStream_t>(stream))
+                           : launch_rows_quant<false>(*g, X, xdt, p, ydt, reinterpret_cast<hipStream_t>(stream));
+    }
     const size_t y_bytes = (size_t)M * (ydt == QARVD_F32 ? 4 : 2);
     const size_t gemm_bytes = (size_t)N * ((size_t)g->kp * w_bits / 8 + y_bytes * (g->R ? 2 : 1));
     return qarvd_quant_act_before_gemm(X, xdt, M, K, ldx, K_o > 0 ? perm : nullptr, K_o, Xq, ld, s_x, gemm_bytes, stream);
@@ -485,9 +520,11 @@ extern "C" qarvd_status qarvd_linear_fused(const void *X, qarvd_dtype xdt, int64
                                            qarvd_dtype ydt, int64_t ldy, void *workspace, size_t workspace_bytes, void *stream)
 {
     GemmArgs g;
-    if (qarvd_status st = quantize_for_gemm(X, xdt, ldx, perm, w_bits, Wq, ldwq, s_normal, s_outlier, bias, ending, M, N, K, K_o, Y, ydt, ldy,
-                                            workspace, workspace_bytes, stream, &g);
-        st != QARVD_OK)
+    bool done = false;
+    const qarvd_ending none = {QARVD_ACT_NONE, M, nullptr, 0, nullptr, 0};
+    if (qarvd_status st = quantize_for_gemm(X, xdt, ldx, perm, w_bits, Wq, ldwq, s_normal, s_outlier, bias, ending ? ending : &none, M, N, K, K_o, Y,
+                                            ydt, ldy, workspace, workspace_bytes, stream, &g, &done);
+        st != QARVD_OK || done)
         return st;
     return launch_fused(w_bits, 0, g, ydt, stream);
 }

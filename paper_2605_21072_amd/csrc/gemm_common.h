@@ -109,6 +109,12 @@ qarvd_status launch_dma128(const GemmArgs &g, qarvd_dtype ydt, hipStream_t st);
 // fused endings (gemm_fused.hip): g.act, g.gate, g.R
 template <int BM, int BN, int WM, int WN, int NSTAGE, bool GEN, bool W4>
 qarvd_status launch_dma128_fused(const GemmArgs &g, qarvd_dtype ydt, hipStream_t st);
+template <int MT, int CT, int P, bool W4>      // up to 16 MT / P rows (gemm_rows.hip)
+qarvd_status launch_rows_gemm(const GemmArgs &g, qarvd_dtype ydt, hipStream_t st);
+// the same from activations that the kernel quantizes itself, for calls that rows_quant_fits
+bool rows_quant_fits(const GemmArgs &g, int cus);
+template <bool W4>
+qarvd_status launch_rows_quant(const GemmArgs &g, const void *X, qarvd_dtype xdt, const int32_t *perm, qarvd_dtype ydt, hipStream_t st);
 template <bool W4>
 qarvd_status launch_staged_fused(const GemmArgs &g, qarvd_dtype ydt, hipStream_t st);
 template <int BM, int BN, int WM, int WN, int NSTAGE, bool DUAL>

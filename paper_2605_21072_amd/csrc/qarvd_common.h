@@ -19,6 +19,11 @@ __attribute__((visibility("hidden")))
 qarvd_status qarvd_quant_act_before_gemm(const void *X, qarvd_dtype xdt, int32_t M, int32_t K, int64_t ldx, const int32_t *perm, int32_t K_o,
                                          int8_t *Xq, int64_t ldxq, float *s_x, size_t gemm_bytes, void *stream);
 
+// The checks of qarvd_quant_act alone (quant_act.hip).
+__attribute__((visibility("hidden")))
+qarvd_status qarvd_quant_act_check(const void *X, qarvd_dtype xdt, int32_t M, int32_t K, int64_t ldx, const int32_t *perm, int32_t K_o,
+                                   const int8_t *Xq, int64_t ldxq, const float *s_x);
+
 // The checks of qarvd_qk_norm_rope alone (heads.hip).
 __attribute__((visibility("hidden")))
 qarvd_status qarvd_heads_check(const qarvd_heads *q, const qarvd_heads *k, qarvd_dtype dt, int32_t M, int32_t D, qarvd_norm norm, float eps,

@@ -446,20 +446,27 @@ qarvd_status dispatch(const ActArgs &a, bool whole_words, hipStream_t st)
     return qarvd_launch_status();
 }
 
-qarvd_status quant_act_common(const void *X, qarvd_dtype xdt, int32_t M, int32_t K, int64_t ldx,
-                              const int32_t *perm, int32_t K_o, int8_t *Xq, int64_t ldxq, float *s_x,
-                              bool is_static, float scale, size_t gemm_bytes, void *stream)
+qarvd_status check_args(const void *X, qarvd_dtype xdt, int32_t M, int32_t K, int64_t ldx, const int32_t *perm, int32_t K_o, const int8_t *Xq,
+                        int64_t ldxq, const float *s_x, bool is_static, float scale)
 {
     if (!X || !Xq || (!is_static && !s_x)) return QARVD_ERR_INVALID_ARG;
     if (M <= 0 || K <= 0 || K > QARVD_MAX_K || K_o < 0 || K_o > K || ldx < K) return QARVD_ERR_INVALID_ARG;
     if (!perm && K_o != 0) return QARVD_ERR_INVALID_ARG;
     if (is_static && !(scale >= 0.0f)) return QARVD_ERR_INVALID_ARG;
-    const PackedK g = qarvd_packed(K, K_o);
-    if (ldxq < g.kp) return QARVD_ERR_INVALID_ARG;
+    if (ldxq < qarvd_packed(K, K_o).kp) return QARVD_ERR_INVALID_ARG;
     if (xdt != QARVD_F32 && xdt != QARVD_BF16) return QARVD_ERR_UNSUPPORTED;
     if (!qarvd_aligned16(Xq) || (ldxq % 16) != 0) return QARVD_ERR_UNSUPPORTED;
+    if (reinterpret_cast<uintptr_t>(X) % (xdt == QARVD_F32 ? 4 : 2)) return QARVD_ERR_UNSUPPORTED;
+    return QARVD_OK;
+}
+
+qarvd_status quant_act_common(const void *X, qarvd_dtype xdt, int32_t M, int32_t K, int64_t ldx,
+                              const int32_t *perm, int32_t K_o, int8_t *Xq, int64_t ldxq, float *s_x,
+                              bool is_static, float scale, size_t gemm_bytes, void *stream)
+{
+    if (qarvd_status s = check_args(X, xdt, M, K, ldx, perm, K_o, Xq, ldxq, s_x, is_static, scale); s != QARVD_OK) return s;
+    const PackedK g = qarvd_packed(K, K_o);
     const size_t esz = xdt == QARVD_F32 ? 4 : 2;
-    if (reinterpret_cast<uintptr_t>(X) % esz) return QARVD_ERR_UNSUPPORTED;
     ActArgs a;
     a.X = X; a.ldx = ldx; a.perm = perm; a.Xq = Xq; a.ldxq = ldxq; a.s_x = s_x; a.static_scale = scale;
     a.M = M; a.K = K; a.K_o = K_o; a.n_off = g.n_off; a.kp = g.kp;
@@ -473,6 +480,12 @@ qarvd_status quant_act_common(const void *X, qarvd_dtype xdt, int32_t M, int32_t
 }
 
 }  // namespace
+
+qarvd_status qarvd_quant_act_check(const void *X, qarvd_dtype xdt, int32_t M, int32_t K, int64_t ldx, const int32_t *perm, int32_t K_o,
+                                   const int8_t *Xq, int64_t ldxq, const float *s_x)
+{
+    return check_args(X, xdt, M, K, ldx, perm, K_o, Xq, ldxq, s_x, false, 0.0f);
+}
 
 qarvd_status qarvd_quant_act_before_gemm(const void *X, qarvd_dtype xdt, int32_t M, int32_t K, int64_t ldx, const int32_t *perm, int32_t K_o,
                                          int8_t *Xq, int64_t ldxq, float *s_x, size_t gemm_bytes, void *stream)

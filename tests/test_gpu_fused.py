@@ -112,6 +112,48 @@ def test_every_kernel_by_number(M, N, K, K_o, dtype):
     assert len(ran) >= (8 if N % 8 == 0 else 6)
 
 
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("N,K,K_o", [(8, 96, 96), (131, 1000, 7), (520, 4200, 160), (2056, 130, 0), (4104, 300, 64), (8200, 260, 33)])
+def test_few_rows(N, K, K_o, bits):
+    """Tokens from one to more than the kernels for few rows take, outputs on either side of what each of them takes."""
+    w, codes = layer(N + K, N, K, K_o, bits)
+    for M in (1, 2, 7, 8, 9, 16, 17, 32, 33):
+        gates = min(M, 3)
+        rows = -(-M // gates)
+        for act, residual, dtype in ((0, True, torch.bfloat16), (1, False, torch.float32)):
+            X, bias, gate, R = inputs(M, M, K, N, dtype, act, gates, residual)
+            Xq, s_x = q.quant_act(X, w.perm if K_o else None, K_o)
+            y, err = definition(Xq, s_x, w, codes, bias)
+            Y = q.w8a8_linear_fused(X, w, bias, act=act, gate=gate, gate_rows=rows, residual=R, out_dtype=dtype)
+            check(Y, y, err, act, gate, rows, R)
+            for v in range(1, q.fused_gemm_num_variants() + 1):
+                try:
+                    got = q.w8a8_dual_gemm_fused(Xq, s_x, w, bias, M, act=act, gate=gate, gate_rows=rows, residual=R, out_dtype=dtype, variant=v)
+                except q.QarvdError as e:
+                    assert e.status == -2
+                    continue
+                assert torch.equal(got, Y), v
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("K,K_o", [(4, 0), (3, 3), (97, 33), (1536, 32), (8960, 64), (10240, 0), (10239, 160), (10240, 10240), (10241, 32)])
+def test_one_token_quantized_on_the_way(K, K_o, bits):
+    """One row is quantized by the GEMM's own workgroups up to 10240 channels: the codes and the scale of quant_act, whatever the row's size."""
+    N = 72
+    w, _ = layer(K, N, K, K_o, bits)
+    gen = torch.Generator(device="cuda").manual_seed(K)
+    for dtype in (torch.float32, torch.bfloat16):
+        row = torch.randn((1, K + 1), generator=gen, device="cuda")
+        row[0, ::7] *= 15
+        for scale in (1.0, 0.0, 1e-36, 1e-30, 3e34, float("inf")):
+            X = (row * scale if scale < 1e38 else row.masked_fill(row > 3, scale)).to(dtype)[:, 1:]       # (an odd address, too)
+            Xq, s_x = q.quant_act(X, w.perm if K_o else None, K_o)
+            bias, R = torch.randn(N, generator=gen, device="cuda"), torch.randn((1, N), generator=gen, device="cuda")
+            want = q.w8a8_dual_gemm_fused(Xq, s_x, w, bias, 1, residual=R, out_dtype=torch.float32)
+            got = q.w8a8_linear_fused(X, w, bias, residual=R, out_dtype=torch.float32)
+            assert torch.equal(got.view(torch.int32), want.view(torch.int32)), (dtype, scale)
+
+
 @pytest.mark.parametrize("M,rows", [(300, 1), (300, 7), (300, 100), (300, 255), (300, 256), (300, 299), (1100, 300), (1100, 520), (40, 40), (40, 1 << 30)])
 def test_groups_of_tokens(M, rows):
     """Groups shorter than a row block, boundaries inside a tile and a wave's rows, one group; the result is the formula's, bit for bit."""
