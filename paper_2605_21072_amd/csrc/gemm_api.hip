@@ -55,11 +55,11 @@ constexpr int kNumVariants = sizeof(kVariants) / sizeof(kVariants[0]);
 
 bool short_rows_ok(const GemmArgs &g) { return g.ldxq <= (1 << 22) && g.ldwq <= (1 << 22); }
 
-bool vector_out_ok(const GemmArgs &g, qarvd_dtype ydt)
+bool vector_out_ok(const GemmArgs &g, qarvd_dtype ydt, int columns = 8)
 {
     const size_t esz = ydt == QARVD_F32 ? 4 : 2;
     // the LDS-direct kernels also address a tile's rows with 32-bit byte offsets: 256 rows x stride x 4 < 2^31
-    return (g.N % 8) == 0 && qarvd_aligned16(g.Y) && ((g.ldy * esz) % 16) == 0 && qarvd_aligned16(g.s_n) &&
+    return (g.N % columns) == 0 && qarvd_aligned16(g.Y) && ((g.ldy * esz) % 16) == 0 && qarvd_aligned16(g.s_n) &&
            qarvd_aligned16(g.s_o) && qarvd_aligned16(g.bias) && short_rows_ok(g) && g.ldy <= (1 << 20);
 }
 
@@ -161,7 +161,7 @@ qarvd_status check_and_fill(int bits, const int8_t *Xq, int64_t ldxq, const floa
     g.Y = Y; g.dbg_n = dbg_acc_normal; g.dbg_o = dbg_acc_outlier;
     g.ldxq = ldxq; g.ldwq = ldwq; g.ldy = ldy; g.M = M; g.N = N; g.n_off = pk.n_off; g.kp = pk.kp;
     g.tiles_m = g.tiles_n = 0; g.act = 0; g.out_scale = 0.0f; g.store_wt = 0;
-    g.gate = nullptr; g.R = nullptr; g.ldg = g.ldr = 0; g.gate_rows = 0x7fffffff;
+    g.gate = nullptr; g.R = nullptr; g.ldg = g.ldr = 0; g.gate_rows = 0x7fffffff; g.last_group = 0;
     g.vec_out = vector_out_ok(g, ydt);
     *out = g;
     return QARVD_OK;
@@ -312,7 +312,7 @@ extern "C" qarvd_status qarvd_w8a8_dual_gemm_q8(const int8_t *Xq, int64_t ldxq, 
     g.Y = Y8; g.dbg_n = nullptr; g.dbg_o = nullptr;
     g.ldxq = ldxq; g.ldwq = ldwq; g.ldy = ldy8; g.M = M; g.N = N; g.n_off = pk.n_off; g.kp = pk.kp;
     g.tiles_m = g.tiles_n = 0; g.act = (int32_t)act; g.out_scale = out_scale; g.vec_out = 1; g.store_wt = 0;
-    g.gate = nullptr; g.R = nullptr; g.ldg = g.ldr = 0; g.gate_rows = 0x7fffffff;
+    g.gate = nullptr; g.R = nullptr; g.ldg = g.ldr = 0; g.gate_rows = 0x7fffffff; g.last_group = 0;
     if (g.n_off > 128) return QARVD_ERR_UNSUPPORTED;
     if (variant == 0) {
         const double T = g.kp / 64;
@@ -371,6 +371,7 @@ constexpr int kNumFusedVariants = sizeof(kFusedVariants) / sizeof(kFusedVariants
 // Checks of an ending beside those of the GEMM, and its part of the kernel arguments.  vec_out then covers the residual and the gate too.
 qarvd_status fill_ending(const qarvd_ending *e, qarvd_dtype ydt, GemmArgs *g)
 {
+    if (ydt == QARVD_F32) g->vec_out = vector_out_ok(*g, ydt, 4);       // four columns are whole 16-byte chunks already
     if (!e) return QARVD_OK;
     if (e->act != QARVD_ACT_NONE && e->act != QARVD_ACT_GELU_TANH) return QARVD_ERR_INVALID_ARG;
     const size_t esz = ydt == QARVD_F32 ? 4 : 2;
@@ -379,6 +380,7 @@ qarvd_status fill_ending(const qarvd_ending *e, qarvd_dtype ydt, GemmArgs *g)
         if (reinterpret_cast<uintptr_t>(e->gate) & 3u) return QARVD_ERR_UNSUPPORTED;
         g->gate = e->gate;
         g->gate_rows = e->gate_rows;
+        g->last_group = (g->M - 1) / e->gate_rows;
         g->ldg = e->gate_rows < g->M ? e->ldg : 0;            // one group: its row alone
         g->vec_out = g->vec_out && qarvd_aligned16(e->gate) && g->ldg % 4 == 0 && g->ldg <= (1 << 20);
     }
@@ -408,6 +410,9 @@ int32_t pick_rows(int bits, const GemmArgs &g)
     return 0;
 }
 
+// The aligned tiles have room for the gates of two groups of tokens.
+bool gates_fit(const FusedVariant &v, const GemmArgs &g) { return v.form != 0 || g.last_group <= 1 || g.gate_rows >= v.BM - 1; }
+
 qarvd_status launch_fused(int bits, int32_t variant, const GemmArgs &g, qarvd_dtype ydt, void *stream)
 {
     if (variant == 0) {
@@ -424,17 +429,20 @@ qarvd_status launch_fused(int bits, int32_t variant, const GemmArgs &g, qarvd_dt
     if (variant == 0) {
         const bool fast_ok = g.n_off <= 128 && g.vec_out;
         // (INT4: the any-width tiles stand beside the aligned ones, as for the plain GEMM)
-        const int form = !short_rows_ok(g) ? 2 : fast_ok ? 0 : 1;
+        const int form = !short_rows_ok(g) ? 2 : fast_ok && (g.last_group <= 1 || g.gate_rows >= 63) ? 0 : 1;      // (64 rows: the lowest tile)
         Cand cand[kNumFusedVariants];
         int n = 0;
+        const bool gelu_alone = !g.gate && !g.R;
         for (int i = 0; i < kNumFusedVariants; ++i) {
             const FusedVariant &v = kFusedVariants[i];
+            if ((v.BM * v.BN > 128 * 256 && !gelu_alone) || !gates_fit(v, g)) continue;
             if (v.bits == bits && (v.form == form || (bits == 4 && form == 0 && v.form == 1))) cand[n++] = {i + 1, v.BM, v.BN, v.c, v.a, v.b};
         }
         variant = cheapest(cand, n, g);
     }
     const FusedVariant &v = kFusedVariants[variant - 1];
-    if (v.bits != bits || (v.form == 0 && !(g.n_off <= 128 && g.vec_out)) || (v.form == 1 && !short_rows_ok(g)) || (v.form == 3 && g.M > v.BM))
+    if (v.bits != bits || (v.form == 0 && !(g.n_off <= 128 && g.vec_out)) || (v.form == 1 && !short_rows_ok(g)) || (v.form == 3 && g.M > v.BM) ||
+        !gates_fit(v, g))
         return QARVD_ERR_UNSUPPORTED;
     return v.launch(g, ydt, reinterpret_cast<hipStream_t>(stream));
 }

@@ -49,7 +49,7 @@ struct GemmArgs {
     const float *gate;
     const void *R;     // of the output's type
     int64_t ldg, ldr;
-    int32_t gate_rows;
+    int32_t gate_rows, last_group;      // last_group = (M - 1) / gate_rows
     int32_t K, K_o;    // as the caller gave them (the kernels go by n_off and kp)
 };
 

@@ -44,9 +44,8 @@
 // END selects what follows the dequantized sum in the epilogue: nothing (ENDING_NONE), the tanh form of GELU, and a gate with a
 // residual, Y = R + g y.  A lane's four values of a 16 x 16 block are one row's four neighbouring columns, so the residual is loaded
 // straight into that layout, 8 bytes (bf16) or 16 a lane: the four blocks of a 64-column row ask for the same lines one after another, and
-// no value passes through LDS twice.  The loads of the first row blocks go out before the next tile's first stage, the others a
-// fixed number of row blocks ahead (RES_AHEAD); the sum is rounded to the output type once.  The gate of a lane's columns stays in registers and is
-// read again in the row blocks of a tile in which the group changes.
+// no value passes through LDS twice.  A wave tile's residual goes out as a whole under the K loop's last iterations, the gates come with the
+// scales; the sum is rounded to the output type once.  256 x 256 tiles have no registers for it.
 #pragma once
 #include <algorithm>
 #include <type_traits>
@@ -73,7 +72,7 @@ __device__ __forceinline__ int swz128(int r) { return ((r >> 1) & 1) | (((r >> 3
 __device__ __forceinline__ int swz_w4(int r) { return (r >> 2) & 3; }
 
 // W4: the W operand is packed INT4, 64 bytes per row and stage.
-template <int BM, int BN, int WM, int WN, int NSTAGE, bool W4>
+template <int BM, int BN, int WM, int WN, int NSTAGE, bool W4, bool RES = false>
 struct Geo2 {
     static constexpr int NW = WM * WN;
     static constexpr int THREADS = 64 * NW;
@@ -85,7 +84,7 @@ struct Geo2 {
     static constexpr int NLOAD = NA + NB;
     static constexpr int STG = BM * BK2 + BN * WROW;
     static constexpr int PATCHES = NW * PATCH2_BYTES;
-    static constexpr int NSCALE = BM + 3 * BN;
+    static constexpr int NSCALE = BM + (RES ? 5 : 3) * BN;         // (RES: the gates of two groups of tokens)
     static constexpr int SCALE_BYTES = 2 * NSCALE * (int)sizeof(float);
     static constexpr bool PATCH_EXTRA = NSTAGE * STG + PATCHES + SCALE_BYTES <= 160 * 1024;   // patches behind the stages
     static constexpr int PATCH_OFF = NSTAGE * STG;
@@ -107,16 +106,17 @@ struct Geo2 {
 // Endings: what the epilogue applies to y, the result of the plain GEMM.
 constexpr int ENDING_NONE = 0, ENDING_GELU = 1, ENDING_RESIDUAL = 2;      // (bits: 3 is both)
 
+typedef v4f v4f_any __attribute__((aligned(4)));
 typedef v4i v4i_unaligned __attribute__((aligned(2)));   // 16 bytes at an address that is aligned to an output element only
 
 // WT: output stores write through the L2 (see output_writes_through).
 template <int BM, int BN, int WM, int WN, int NSTAGE, bool DUAL, bool DBG, typename OutT, bool GEN, bool W4, bool WT, int END>
-__global__ __launch_bounds__(64 * WM * WN, (Geo2<BM, BN, WM, WN, NSTAGE, W4>::WAVES_PER_SIMD)) void gemm_dma128_kernel(GemmArgs g)
+__global__ __launch_bounds__(64 * WM * WN, (Geo2<BM, BN, WM, WN, NSTAGE, W4, (END & ENDING_RESIDUAL) != 0>::WAVES_PER_SIMD)) void gemm_dma128_kernel(GemmArgs g)
 {
-    using G = Geo2<BM, BN, WM, WN, NSTAGE, W4>;
+    using G = Geo2<BM, BN, WM, WN, NSTAGE, W4, (END & ENDING_RESIDUAL) != 0>;
     constexpr int TM = G::TM, TN = G::TN, NA = G::NA, NB = G::NB, NW = G::NW, STG = G::STG, NL = G::NLOAD;
     extern __shared__ __align__(16) unsigned char smem[];
-    float *const sc_both = reinterpret_cast<float *>(smem + G::SCALES_OFF);   // 2 x { s_x[BM] | s_n[BN] | s_o[BN] | bias[BN] }
+    float *const sc_both = reinterpret_cast<float *>(smem + G::SCALES_OFF);   // 2 x { s_x[BM] | s_n[BN] | s_o[BN] | bias[BN] | RES: gate[2][BN] }
 
     const long long p_ts = QARVD_PROF ? clock64() : 0;
     const long long p_rs = QARVD_PROF ? wall_clock64() : 0;
@@ -166,20 +166,26 @@ __global__ __launch_bounds__(64 * WM * WN, (Geo2<BM, BN, WM, WN, NSTAGE, W4>::WA
     constexpr int ESZ = (int)sizeof(OutT);
     constexpr bool RES = (END & ENDING_RESIDUAL) != 0;
     using res_t = std::conditional_t<sizeof(OutT) == 4, v4f, v2u>;            // four elements of R
+    typedef res_t res_any __attribute__((aligned(2)));
     static_assert(END == ENDING_NONE || sizeof(OutT) > 1, "INT8 outputs have an ending of their own");
-    constexpr int RES_AHEAD = RES ? std::max(1, std::min(TM, (TM * TN >= 32 ? 8 : TM * TN >= 16 ? 16 : 32) / (TN * (int)sizeof(res_t) / 4))) : 1;     // row blocks in flight
+    static_assert(!RES || TM * TN <= 16, "registers for a whole wave tile of the residual");
 
     // ---- scales and bias: registers during the previous tile's K loop, then the other LDS buffer ----
     float r_s[G::SPT];
     auto fetch_scales = [&](int sm0, int sn0) {
+        [[maybe_unused]] const int s_group = RES ? (int)((unsigned)sm0 / (unsigned)g.gate_rows) : 0;
 #pragma unroll
         for (int u = 0; u < G::SPT; ++u) {
             const int e = tid + u * G::THREADS;
             float v = 0.f;
             if (e < BM) v = g.s_x[min(sm0 + e, g.M - 1)];
             else if (e < BM + BN) v = g.s_n[min(sn0 + e - BM, g.N - 1)] * (W4 ? 0.0625f : 1.0f);             // INT4 codes enter the
-            else if (e < BM + 2 * BN) v = g.s_o[min(sn0 + e - BM - BN, g.N - 1)] * (W4 ? 0.0625f : 1.0f);    // MFMA times 16 (exact)
-            else if (e < BM + 3 * BN && g.bias) v = g.bias[min(sn0 + e - BM - 2 * BN, g.N - 1)];
+            else if (e < BM + 2 * BN) v = RES && g.n_off == 0 ? 0.f : g.s_o[min(sn0 + e - BM - BN, g.N - 1)] * (W4 ? 0.0625f : 1.0f);    // MFMA times 16 (exact)
+            else if (e < BM + 3 * BN) v = g.bias ? g.bias[min(sn0 + e - BM - 2 * BN, g.N - 1)] : 0.f;
+            else if (RES && e < G::NSCALE) {       // of the group of the tile's first row and of the next (there is one, or the same again)
+                const int c = e - BM - 3 * BN;
+                v = g.gate ? g.gate[(size_t)min(s_group + (c >= BN ? 1 : 0), g.last_group) * g.ldg + min(sn0 + (c & (BN - 1)), g.N - 1)] : 1.0f;
+            }
             r_s[u] = v;
         }
     };
@@ -307,6 +313,85 @@ __global__ __launch_bounds__(64 * WM * WN, (Geo2<BM, BN, WM, WN, NSTAGE, W4>::WA
     int stage = base;
     [[maybe_unused]] const long long p_t0 = QARVD_PROF ? clock64() : 0;
 
+    // Residual of block (i, j), rows lr and columns 4 lq .. + 3 of it.  The descriptor covers the rows of the tile that exist (none without a
+    // residual: zeros are added); columns past the matrix read what lies there inside those rows, or zeros, and are never stored.
+    [[maybe_unused]] res_t rs[RES ? TM : 1][RES ? TN : 1];
+    [[maybe_unused]] int r_lane = 0, r_bytes = 0, lr = 0, lq = 0;
+    [[maybe_unused]] const int ldr_b = RES ? (int)g.ldr * ESZ : 0;
+    auto load_residual = [&](int i, int j) {
+        if constexpr (RES) {
+            if (!GEN || g.vec_out) {
+                rs[i][j] = buffer_load_as<res_t>(reinterpret_cast<const OutT *>(g.R) + (size_t)m0 * g.ldr, r_bytes, r_lane, i * 16 * ldr_b + j * 16 * ESZ);
+            } else {
+                const int row = wm * G::WTM + i * 16 + lr, left = g.N - (n0 + wn * G::WTN + j * 16 + 4 * lq);
+                const OutT *const r = reinterpret_cast<const OutT *>(g.R) + (size_t)(m0 + row) * g.ldr + (g.N - left);
+                OutT e[4] = {0, 0, 0, 0};
+                if (g.R && m0 + row < g.M) {
+                    if (left >= 4) {
+                        rs[i][j] = *reinterpret_cast<const res_any *>(r);
+                        return;
+                    }
+#pragma unroll
+                    for (int k = 0; k < 3; ++k)
+                        if (k < left) e[k] = r[k];
+                }
+                rs[i][j] = pack4(e);
+            }
+        }
+    };
+    // Gate of this lane's columns of block (i, j).  A tile whose rows are of two groups at most, as where a group has BM - 1 tokens or more,
+    // has them in LDS with its scales: a load in the epilogue would wait, in order, for the output stores in front of it.  GEN takes groups of any
+    // size; what does not fit is loaded.
+    [[maybe_unused]] v4f gt[RES ? TN : 1];
+    [[maybe_unused]] int next_group = 0;            // row of the tile from which the second group's tokens stand
+    [[maybe_unused]] const bool gates_in_lds = !GEN || g.last_group <= 1 || g.gate_rows >= BM - 1;
+    auto load_gate = [&](int i, int j, const float *gate_lds) {
+        if constexpr (RES) {
+            const int row = wm * G::WTM + i * 16 + lr, nt = wn * G::WTN + j * 16 + 4 * lq;
+            if (gates_in_lds) {
+                gt[j] = *reinterpret_cast<const v4f *>(gate_lds + (row >= next_group ? BN : 0) + nt);
+            } else {
+                const float *const gr = g.gate + (size_t)((unsigned)min(m0 + row, g.M - 1) / (unsigned)g.gate_rows) * g.ldg;
+                const int col = n0 + nt;
+                if (col + 4 <= g.N) {
+                    gt[j] = *reinterpret_cast<const v4f_any *>(gr + col);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) gt[j][k] = gr[min(col + k, g.N - 1)];
+                }
+            }
+        }
+    };
+    auto aim_ending = [&](int row, int quarter) {   // for the tile at (m0, n0)
+        lr = row;
+        lq = quarter;
+        r_lane = (wm * G::WTM + lr) * ldr_b + (n0 + wn * G::WTN + 4 * lq) * ESZ;
+        r_bytes = g.R ? (min(BM, g.M - m0) - 1) * ldr_b + g.N * ESZ : 0;
+        const int first = (int)__builtin_amdgcn_readfirstlane((unsigned)m0 / (unsigned)g.gate_rows);
+        next_group = (int)min((int64_t)(first + 1) * g.gate_rows - m0, (int64_t)BM);
+    };
+    // The whole wave tile's residual goes out in front of the K loop's last iterations, behind all stage loads, whose waits leave it in
+    // flight; where the number of loads differs from wave to wave (edges of a GEN tile), after the loop.  (Spread over the loop, at another
+    // place in every tile, it cost up to 1 us more.)
+    constexpr int YOUNGER = RES ? TM * TN : 0;
+    [[maybe_unused]] const bool early = RES && (!GEN || g.vec_out);
+    auto load_ending = [&](int row, int quarter) {
+        aim_ending(row, quarter);
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) load_residual(i, j);
+    };
+    auto begin_tail = [&]() {
+        if constexpr (RES) {
+            if (early) load_ending(frow, fq);
+        }
+    };
+    auto wait_tail = [&](int stages) {
+        if (RES && early) wait_stages_in_flight<NSTAGE - 2, NL, YOUNGER>(stages);
+        else wait_stages_in_flight<NSTAGE - 2, NL>(stages);
+    };
+
     // iteration it:  MFMA F0 | read F1 under it;  wait, barrier;  MFMA F1 | read F0(it+1), refill this stage with K tile it+NSTAGE
     // Before the barrier a wave waits for its own loads of stage it+1 and for its own LDS reads (the last
     // fragments of this stage), so after the barrier stage it+1 is complete and stage `it` is dead.
@@ -375,11 +460,12 @@ __global__ __launch_bounds__(64 * WM * WN, (Geo2<BM, BN, WM, WN, NSTAGE, W4>::WA
             first_half();
             refill_half(it + NSTAGE);
         }
+        begin_tail();
 #pragma unroll 1
         for (; it < T; ++it) {
             first_half();
             if (it + 1 < T) {
-                wait_stages_in_flight<NSTAGE - 2, NL>(T - 2 - it);
+                wait_tail(T - 2 - it);
                 wait_lgkmcnt0();
                 __builtin_amdgcn_s_barrier();
                 load_frags(smem + next_of(stage) * STG, 0);
@@ -395,10 +481,11 @@ __global__ __launch_bounds__(64 * WM * WN, (Geo2<BM, BN, WM, WN, NSTAGE, W4>::WA
             refill_half(seq(it + NSTAGE));
         }
         // the last tiles, nothing left to issue
+        begin_tail();
 #pragma unroll 1
         for (; it < T - 1; ++it) {
             first_half();
-            wait_stages_in_flight<NSTAGE - 2, NL>(T - 2 - it);       // stage it + 1 has landed
+            wait_tail(T - 2 - it);                                   // stage it + 1 has landed
             wait_lgkmcnt0();
             __builtin_amdgcn_s_barrier();
             load_frags(smem + next_of(stage) * STG, 0);
@@ -426,64 +513,8 @@ __global__ __launch_bounds__(64 * WM * WN, (Geo2<BM, BN, WM, WN, NSTAGE, W4>::WA
     int el = lane;
     asm volatile("" : "+v"(el));
     const int er = el & 15, eq = el >> 4;
-    // Residual of block (i, j).  The descriptor covers the rows of the tile that exist (none without a residual: zeros are added);
-    // columns past the matrix read what lies there inside those rows, or zeros, and are never stored.
-    [[maybe_unused]] res_t rs[RES_AHEAD][RES ? TN : 1];
-    [[maybe_unused]] const int ldr_b = RES ? (int)g.ldr * ESZ : 0, r_bytes = RES && g.R ? (min(BM, g.M - m0) - 1) * ldr_b + g.N * ESZ : 0;
-    [[maybe_unused]] const OutT *const r_tile = reinterpret_cast<const OutT *>(g.R) + (RES ? (size_t)m0 * g.ldr : 0);
-    [[maybe_unused]] const int r_lane = (wm * G::WTM + er) * ldr_b + (n0 + wn * G::WTN + 4 * eq) * ESZ;
-    auto load_residual = [&](int i, int j) {
-        if constexpr (RES) {
-            if (!GEN || g.vec_out) {
-                rs[i % RES_AHEAD][j] = buffer_load_as<res_t>(r_tile, r_bytes, r_lane, i * 16 * ldr_b + j * 16 * ESZ);
-            } else {
-                const int row = wm * G::WTM + i * 16 + er, col = n0 + wn * G::WTN + j * 16 + 4 * eq;
-                const OutT *const r = reinterpret_cast<const OutT *>(g.R) + (size_t)(m0 + row) * g.ldr + col;
-                OutT e[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) e[k] = g.R && m0 + row < g.M && col + k < g.N ? r[k] : (OutT)0;
-                rs[i % RES_AHEAD][j] = pack4(e);
-            }
-        }
-    };
-    // Gate of this lane's columns of block (i, j), from the row of its token's group (rows past the matrix: that of the last).  The groups
-    // are counted from that of the tile's first row: the fp32 quotient is off by at most 2^-22 of itself, less than its distance
-    // from the next whole number, 0.5 / gate_rows, because a group longer than 2^20 is counted as if it had 2^20 rows, its last
-    // ones (a tile then reaches into one more at most).  Without a gate the descriptor is empty and gate_add is 1.
-    [[maybe_unused]] v4f gt[RES ? TN : 1];
-    [[maybe_unused]] const unsigned gate_first = RES ? __builtin_amdgcn_readfirstlane((unsigned)m0 / (unsigned)g.gate_rows) : 0;
-    [[maybe_unused]] const int gate_rows = min(g.gate_rows, 1 << 20);
-    [[maybe_unused]] const int gate_row0 = m0 - (int)(gate_first * (unsigned)g.gate_rows) - (g.gate_rows - gate_rows);
-    [[maybe_unused]] const float gate_add = RES && !g.gate ? 1.0f : 0.0f, gate_rcp = RES ? 1.0f / (float)gate_rows : 0.0f;
-    auto gate_group = [&](int row) {                // of a row of the tile
-        return (int)(((float)max(gate_row0 + min(row, g.M - 1 - m0), 0) + 0.5f) * gate_rcp);
-    };
-    [[maybe_unused]] const float *const gate_tile = g.gate + (RES ? (size_t)gate_first * g.ldg : 0);
-    [[maybe_unused]] const int gate_bytes = RES && g.gate ? (__builtin_amdgcn_readfirstlane(gate_group(BM - 1)) * (int)g.ldg + g.N) * 4 : 0;      // (scalar: a descriptor in vector registers is a loop)
-    [[maybe_unused]] int gate_lane = 0;
-    auto load_gate = [&](int i, int j) {
-        if constexpr (RES) {
-            if (j == 0) {
-                int row = wm * G::WTM + i * 16 + er;
-                asm volatile("" : "+v"(row));       // (the offsets of all row blocks, computed ahead, would take registers that spill)
-                gate_lane = (gate_group(row) * (int)g.ldg + n0 + wn * G::WTN + 4 * eq) * 4;
-            }
-            if (!GEN || g.vec_out) {
-                gt[j] = buffer_load_as<v4f>(gate_tile, gate_bytes, gate_lane, j * 64);
-            } else {
-                const int row = wm * G::WTM + i * 16 + er, col = n0 + wn * G::WTN + j * 16 + 4 * eq;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) gt[j][k] = g.gate ? gate_tile[(size_t)gate_group(row) * g.ldg + min(col + k, g.N - 1)] : 0.0f;
-            }
-        }
-    };
     if constexpr (RES) {
-#pragma unroll
-        for (int i = 0; i < RES_AHEAD; ++i)
-#pragma unroll
-            for (int j = 0; j < TN; ++j) load_residual(i, j);
-#pragma unroll
-        for (int j = 0; j < TN; ++j) load_gate(0, j);
+        if (!early) load_ending(er, eq);
     }
     const int hstage0 = (base + Tn) % NSTAGE;
     const int pstage = (base + Tn - 1 + 2 * NSTAGE) % NSTAGE;
@@ -495,6 +526,7 @@ __global__ __launch_bounds__(64 * WM * WN, (Geo2<BM, BN, WM, WN, NSTAGE, W4>::WA
     }
     const float *sc_lds = sc_both + sbuf * G::NSCALE;
     const float *sx_lds = sc_lds, *sn_lds = sc_lds + BM, *so_lds = sc_lds + BM + BN, *bs_lds = sc_lds + BM + 2 * BN;
+    [[maybe_unused]] const float *gate_lds = sc_lds + BM + 3 * BN;
     unsigned char *const patch = (G::PATCH_EXTRA ? smem + G::PATCH_OFF : smem + pstage * STG) + wave * PATCH2_BYTES;
     OutT *Y = reinterpret_cast<OutT *>(g.Y);
     constexpr int EPC = 16 / ESZ;     // output elements per 16-byte chunk
@@ -581,18 +613,13 @@ __global__ __launch_bounds__(64 * WM * WN, (Geo2<BM, BN, WM, WN, NSTAGE, W4>::WA
             pending = true;
         };
 
-        // (with 128 accumulator registers, a gate and a residual they are read again for each block: the registers are not there)
-        constexpr bool REREAD = RES && TM * TN >= 32;
         v4f sn[TN], so[TN], bs[TN];
-        auto read_scales = [&](int j) {
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
             const int nt = wn * G::WTN + j * 16 + 4 * eq;             // column inside the workgroup tile
             sn[j] = *reinterpret_cast<const v4f *>(sn_lds + nt);
             if constexpr (HASO) so[j] = *reinterpret_cast<const v4f *>(so_lds + nt);
             bs[j] = *reinterpret_cast<const v4f *>(bs_lds + nt);
-        };
-        if constexpr (!REREAD) {
-#pragma unroll
-            for (int j = 0; j < TN; ++j) read_scales(j);
         }
         // The outlier sum of a block is multiplied while the block before it is worked on, from fragments read a row of blocks
         // ahead.  Half k-steps past the end of the outlier range multiply by zero in the X fragment.
@@ -601,9 +628,9 @@ __global__ __launch_bounds__(64 * WM * WN, (Geo2<BM, BN, WM, WN, NSTAGE, W4>::WA
         const int keep0 = o_steps > (eq >> 1) ? -1 : 0, keep1 = o_steps > 2 + (eq >> 1) ? -1 : 0;
         constexpr bool HOLD = HEAD && OSTEPS == 1 && !RES;      // the W fragments stay in registers, where there is room for them
         v4i wh[HOLD ? TN : 1], xo0, xo1, xn0 = zero4, xn1 = zero4, ao_next = zero4;
-        auto read_head = [&](int i) {
-            if constexpr (HEAD) xn0 = read_x(hb, i, coff[0]) & keep0;
-            if constexpr (HEAD && OSTEPS > 1) xn1 = read_x(hb, i, coff[1]) & keep1;
+        auto read_head = [&](int i, v4i &x0, v4i &x1) {
+            if constexpr (HEAD) x0 = read_x(hb, i, coff[0]) & keep0;
+            if constexpr (HEAD && OSTEPS > 1) x1 = read_x(hb, i, coff[1]) & keep1;
         };
         auto head_mma = [&](int j) {
             if constexpr (HEAD) ao_next = __builtin_amdgcn_mfma_i32_16x16x64_i8(HOLD ? wh[HOLD ? j : 0] : read_w(hb, j, wcoff[0]), xo0, zero4, 0, 0, 0);
@@ -613,9 +640,7 @@ __global__ __launch_bounds__(64 * WM * WN, (Geo2<BM, BN, WM, WN, NSTAGE, W4>::WA
 #pragma unroll
             for (int j = 0; j < TN; ++j) wh[j] = read_w(hb, j, wcoff[0]);
         }
-        read_head(0);
-        xo0 = xn0;
-        xo1 = xn1;
+        read_head(0, xo0, xo1);
         head_mma(0);
         float sx_next = sx_lds[wm * G::WTM + er];
 #pragma unroll
@@ -623,7 +648,7 @@ __global__ __launch_bounds__(64 * WM * WN, (Geo2<BM, BN, WM, WN, NSTAGE, W4>::WA
             const float sx = sx_next;
             if (i + 1 < TM) {
                 sx_next = sx_lds[wm * G::WTM + (i + 1) * 16 + er];
-                read_head(i + 1);
+                if constexpr (!RES) read_head(i + 1, xn0, xn1);
             }
 #pragma unroll
             for (int j = 0; j < TN; ++j) {
@@ -632,13 +657,18 @@ __global__ __launch_bounds__(64 * WM * WN, (Geo2<BM, BN, WM, WN, NSTAGE, W4>::WA
                     ao = acc_o[i][j];
                 } else {
                     ao = ao_next;
-                    if (j == TN - 1) {
-                        xo0 = xn0;
-                        xo1 = xn1;
+                    if constexpr (!RES) {
+                        if (j == TN - 1) {
+                            xo0 = xn0;
+                            xo1 = xn1;
+                        }
                     }
                     if (i + 1 < TM || j + 1 < TN) head_mma((j + 1) % TN);
+                    if constexpr (RES) {           // (no registers for a second set: the next row's as soon as this one's last is multiplied)
+                        if (j == TN - 2 && i + 1 < TM) read_head(i + 1, xo0, xo1);
+                    }
                 }
-                if constexpr (REREAD) read_scales(j);
+                load_gate(i, j, gate_lds);
                 float y[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -652,11 +682,7 @@ __global__ __launch_bounds__(64 * WM * WN, (Geo2<BM, BN, WM, WN, NSTAGE, W4>::WA
                     }
                     y[e] = fmaf(v, sx, bs[j][e]);
                     if constexpr ((END & ENDING_GELU) != 0) y[e] = gelu_tanh(y[e]);
-                    if constexpr (RES) y[e] = fmaf(gt[j][e] + gate_add, y[e], element(rs[i % RES_AHEAD][j], e));
-                }
-                if constexpr (RES) {               // into the registers that this block has just used
-                    if (i + 1 < TM) load_gate(i + 1, j);
-                    if (i + RES_AHEAD < TM) load_residual(i + RES_AHEAD, j);
+                    if constexpr (RES) y[e] = fmaf(gt[j][e], y[e], element(rs[i][j], e));
                 }
                 if constexpr (DBG) {
                     const int m = m0 + wm * G::WTM + i * 16 + er, n = n0 + wn * G::WTN + j * 16 + 4 * eq;
@@ -687,11 +713,13 @@ __global__ __launch_bounds__(64 * WM * WN, (Geo2<BM, BN, WM, WN, NSTAGE, W4>::WA
                 }
                 if (i % PRB == PRB - 1 && j % PCB == PCB - 1) flush(i / PRB * PROWS, j / PCB * PCB * 16);
             }
-            if constexpr (RES) __builtin_amdgcn_sched_barrier(0);     // (without, loads move up into registers that spill)
         }
         flush_commit();
     };
-    if (!DUAL || o_steps == 0) epilogue(std::integral_constant<int, 0>{});
+    // (RES: one form for all, which multiplies what is not there by zero: of a choice among three the compiler keeps a way past all of them, on which the
+    // residual's loads never land, and then waits for everything in flight in each iteration of the K loop)
+    if constexpr (RES) epilogue(std::integral_constant<int, GEN ? 1 : 2>{});
+    else if (!DUAL || o_steps == 0) epilogue(std::integral_constant<int, 0>{});
     else if (GEN || o_steps <= 2) epilogue(std::integral_constant<int, DUAL ? 1 : 0>{});
     else epilogue(std::integral_constant<int, DUAL && !GEN ? 2 : 0>{});
 #if QARVD_PROF
@@ -738,7 +766,7 @@ bool output_writes_through(const GemmArgs &g, size_t elem)
 template <int BM, int BN, int WM, int WN, int NSTAGE, bool DUAL, bool DBG, typename OutT, bool GEN, bool W4, bool WT = true, int END = ENDING_NONE>
 qarvd_status launch128_one(const GemmArgs &g, hipStream_t st)
 {
-    using G = Geo2<BM, BN, WM, WN, NSTAGE, W4>;
+    using G = Geo2<BM, BN, WM, WN, NSTAGE, W4, (END & ENDING_RESIDUAL) != 0>;
     // (the smaller tiles are not chosen for outputs that large, and a dump of the accumulators is not timed)
     if constexpr (WT && BM >= 128 && !DBG && sizeof(OutT) > 1)
         if (!output_writes_through(g, sizeof(OutT))) return launch128_one<BM, BN, WM, WN, NSTAGE, DUAL, DBG, OutT, GEN, W4, false, END>(g, st);

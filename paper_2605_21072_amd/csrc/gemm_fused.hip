@@ -11,12 +11,15 @@ qarvd_status launch_dma128_fused(const GemmArgs &g0, qarvd_dtype ydt, hipStream_
     GemmArgs g = g0;
     g.tiles_m = (g.M + BM - 1) / BM;
     g.tiles_n = (g.N + BN - 1) / BN;
-    const bool gelu = g.act == QARVD_ACT_GELU_TANH, res = g.gate || g.R;
+    const bool gelu = g.act == QARVD_ACT_GELU_TANH, res = g.gate || g.R || !gelu;
     auto as = [&](auto out) {
         using OutT = decltype(out);
         if (!res) return launch128_one<BM, BN, WM, WN, NSTAGE, true, false, OutT, GEN, W4, true, ENDING_GELU>(g, st);
-        if (!gelu) return launch128_one<BM, BN, WM, WN, NSTAGE, true, false, OutT, GEN, W4, true, ENDING_RESIDUAL>(g, st);
-        return launch128_one<BM, BN, WM, WN, NSTAGE, true, false, OutT, GEN, W4, true, ENDING_GELU | ENDING_RESIDUAL>(g, st);
+        if constexpr (BM * BN <= 128 * 256) {
+            if (!gelu) return launch128_one<BM, BN, WM, WN, NSTAGE, true, false, OutT, GEN, W4, true, ENDING_RESIDUAL>(g, st);
+            return launch128_one<BM, BN, WM, WN, NSTAGE, true, false, OutT, GEN, W4, true, ENDING_GELU | ENDING_RESIDUAL>(g, st);
+        }
+        return QARVD_ERR_UNSUPPORTED;       // no registers for the residual of a 256 x 256 tile
     };
     return ydt == QARVD_BF16 ? as(uint16_t{}) : as(float{});
 }

@@ -164,9 +164,16 @@ def test_groups_of_tokens(M, rows):
     Xq, s_x = q.quant_act(X, w.perm, 32)
     y = q.w8a8_dual_gemm(Xq, s_x, w, bias, M, torch.float32).double()
     want = (y * gate.double()[torch.arange(M, device="cuda") // rows] + R.double()).float()       # the fp32 product is exact in 64 bits
+    ran = 0
     for v in range(q.fused_gemm_num_variants() + 1):
-        if v == 0 or v <= 10:
-            assert torch.equal(q.w8a8_dual_gemm_fused(Xq, s_x, w, bias, M, gate=gate, gate_rows=rows, residual=R, out_dtype=torch.float32, variant=v), want), v
+        try:
+            got = q.w8a8_dual_gemm_fused(Xq, s_x, w, bias, M, gate=gate, gate_rows=rows, residual=R, out_dtype=torch.float32, variant=v)
+        except q.QarvdError as e:
+            assert e.status == -2 and v > 0
+            continue
+        ran += 1
+        assert torch.equal(got, want), v
+    assert ran >= (9 if rows >= 255 or groups <= 2 else 5)         # (many short groups: the general kernels and the heuristic)
 
 
 def test_without_an_ending_it_is_the_plain_linear():
