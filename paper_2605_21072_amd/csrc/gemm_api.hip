@@ -336,35 +336,36 @@ struct FusedVariant {
     int BM, BN, bits;
     int form;           // 0: as the aligned tiles need it, 1: strides up to 2^22, 2: anything, 3: at most BM rows
     double c, a, b;     // cost model of pick_variant
+    double gelu, res;   // what GELU, or a gate and a residual, add to a tile's epilogue (a)
     qarvd_status (*launch)(const GemmArgs &, qarvd_dtype, hipStream_t);
 };
-// The tiles and cost constants of the plain GEMMs: an ending adds to a tile's epilogue what it adds to every other's.
+// The tiles and cost constants of the plain GEMMs.
 const FusedVariant kFusedVariants[] = {
-    {256, 256, 8, 0, 0.50, 7.85, 0.539, launch_dma128_fused<256, 256, 2, 4, 2, false, false>},
-    {256, 128, 8, 0, 0.60, 5.81, 0.314, launch_dma128_fused<256, 128, 4, 2, 3, false, false>},
-    {128, 256, 8, 0, 0.55, 5.40, 0.333, launch_dma128_fused<128, 256, 2, 4, 3, false, false>},
-    {128, 128, 8, 0, 1.30, 3.60, 0.183, launch_dma128_fused<128, 128, 2, 4, 3, false, false>},
-    {64, 128, 8, 0, 1.91, 2.35, 0.157, launch_dma128_fused<64, 128, 2, 4, 4, false, false>},
-    {64, 64, 8, 0, 2.40, 0.77, 0.083, launch_dma128_fused<64, 64, 2, 2, 4, false, false>},
-    {128, 128, 8, 1, 1.69, 4.01, 0.181, launch_dma128_fused<128, 128, 2, 4, 3, true, false>},
-    {64, 128, 8, 1, 1.62, 2.97, 0.131, launch_dma128_fused<64, 128, 2, 4, 4, true, false>},
-    {64, 64, 8, 1, 3.13, 0.98, 0.088, launch_dma128_fused<64, 64, 2, 2, 4, true, false>},
-    {128, 128, 8, 2, 0, 0, 0, launch_staged_fused<false>},
-    {256, 256, 4, 0, 2.80, 8.00, 0.517, launch_dma128_fused<256, 256, 2, 4, 3, false, true>},
-    {256, 128, 4, 0, 1.59, 4.44, 0.366, launch_dma128_fused<256, 128, 4, 2, 3, false, true>},
-    {128, 256, 4, 0, 1.29, 4.79, 0.357, launch_dma128_fused<128, 256, 2, 4, 3, false, true>},
-    {128, 128, 4, 1, 2.74, 3.47, 0.196, launch_dma128_fused<128, 128, 2, 4, 3, true, true>},
-    {64, 64, 4, 1, 3.60, 1.00, 0.101, launch_dma128_fused<64, 64, 2, 2, 3, true, true>},
-    {128, 128, 4, 2, 0, 0, 0, launch_staged_fused<true>},
-    {8, 8, 8, 3, 0, 0, 0, launch_rows_gemm<1, 1, 2, false>},
-    {16, 16, 8, 3, 0, 0, 0, launch_rows_gemm<1, 1, 1, false>},
-    {16, 32, 8, 3, 0, 0, 0, launch_rows_gemm<1, 2, 1, false>},
-    {32, 16, 8, 3, 0, 0, 0, launch_rows_gemm<2, 1, 1, false>},
-    {8, 8, 4, 3, 0, 0, 0, launch_rows_gemm<1, 1, 2, true>},
-    {16, 16, 4, 3, 0, 0, 0, launch_rows_gemm<1, 1, 1, true>},
-    {16, 32, 4, 3, 0, 0, 0, launch_rows_gemm<1, 2, 1, true>},
-    {32, 16, 4, 3, 0, 0, 0, launch_rows_gemm<2, 1, 1, true>},
-    {32, 32, 4, 3, 0, 0, 0, launch_rows_gemm<2, 2, 1, true>},
+    {256, 256, 8, 0, 0.50, 7.85, 0.539, 2.8, 0, launch_dma128_fused<256, 256, 2, 4, 2, false, false>},
+    {256, 128, 8, 0, 0.60, 5.81, 0.314, 0.8, 3.2, launch_dma128_fused<256, 128, 4, 2, 3, false, false>},
+    {128, 256, 8, 0, 0.55, 5.40, 0.333, 0.8, 3.1, launch_dma128_fused<128, 256, 2, 4, 3, false, false>},
+    {128, 128, 8, 0, 1.30, 3.60, 0.183, 0.6, 2.4, launch_dma128_fused<128, 128, 2, 4, 3, false, false>},
+    {64, 128, 8, 0, 1.91, 2.35, 0.157, 0.3, 0.5, launch_dma128_fused<64, 128, 2, 4, 4, false, false>},
+    {64, 64, 8, 0, 2.40, 0.77, 0.083, 0.1, 1.0, launch_dma128_fused<64, 64, 2, 2, 4, false, false>},
+    {128, 128, 8, 1, 1.69, 4.01, 0.181, 0.6, 2.4, launch_dma128_fused<128, 128, 2, 4, 3, true, false>},
+    {64, 128, 8, 1, 1.62, 2.97, 0.131, 0.3, 0.5, launch_dma128_fused<64, 128, 2, 4, 4, true, false>},
+    {64, 64, 8, 1, 3.13, 0.98, 0.088, 0.1, 1.0, launch_dma128_fused<64, 64, 2, 2, 4, true, false>},
+    {128, 128, 8, 2, 0, 0, 0, 0, 0, launch_staged_fused<false>},
+    {256, 256, 4, 0, 2.80, 8.00, 0.517, 2.8, 0, launch_dma128_fused<256, 256, 2, 4, 3, false, true>},
+    {256, 128, 4, 0, 1.59, 4.44, 0.366, 0.8, 3.2, launch_dma128_fused<256, 128, 4, 2, 3, false, true>},
+    {128, 256, 4, 0, 1.29, 4.79, 0.357, 0.8, 3.1, launch_dma128_fused<128, 256, 2, 4, 3, false, true>},
+    {128, 128, 4, 1, 2.74, 3.47, 0.196, 0.6, 2.4, launch_dma128_fused<128, 128, 2, 4, 3, true, true>},
+    {64, 64, 4, 1, 3.60, 1.00, 0.101, 0.1, 1.0, launch_dma128_fused<64, 64, 2, 2, 3, true, true>},
+    {128, 128, 4, 2, 0, 0, 0, 0, 0, launch_staged_fused<true>},
+    {8, 8, 8, 3, 0, 0, 0, 0, 0, launch_rows_gemm<1, 1, 2, false>},
+    {16, 16, 8, 3, 0, 0, 0, 0, 0, launch_rows_gemm<1, 1, 1, false>},
+    {16, 32, 8, 3, 0, 0, 0, 0, 0, launch_rows_gemm<1, 2, 1, false>},
+    {32, 16, 8, 3, 0, 0, 0, 0, 0, launch_rows_gemm<2, 1, 1, false>},
+    {8, 8, 4, 3, 0, 0, 0, 0, 0, launch_rows_gemm<1, 1, 2, true>},
+    {16, 16, 4, 3, 0, 0, 0, 0, 0, launch_rows_gemm<1, 1, 1, true>},
+    {16, 32, 4, 3, 0, 0, 0, 0, 0, launch_rows_gemm<1, 2, 1, true>},
+    {32, 16, 4, 3, 0, 0, 0, 0, 0, launch_rows_gemm<2, 1, 1, true>},
+    {32, 32, 4, 3, 0, 0, 0, 0, 0, launch_rows_gemm<2, 2, 1, true>},
 };
 constexpr int kNumFusedVariants = sizeof(kFusedVariants) / sizeof(kFusedVariants[0]);
 
@@ -436,7 +437,7 @@ qarvd_status launch_fused(int bits, int32_t variant, const GemmArgs &g, qarvd_dt
         for (int i = 0; i < kNumFusedVariants; ++i) {
             const FusedVariant &v = kFusedVariants[i];
             if ((v.BM * v.BN > 128 * 256 && !gelu_alone) || !gates_fit(v, g)) continue;
-            if (v.bits == bits && (v.form == form || (bits == 4 && form == 0 && v.form == 1))) cand[n++] = {i + 1, v.BM, v.BN, v.c, v.a, v.b};
+            if (v.bits == bits && (v.form == form || (bits == 4 && form == 0 && v.form == 1))) cand[n++] = {i + 1, v.BM, v.BN, v.c, v.a + (g.act == QARVD_ACT_GELU_TANH ? v.gelu : 0.0) + (gelu_alone ? 0.0 : v.res), v.b};
         }
         variant = cheapest(cand, n, g);
     }

@@ -42,9 +42,10 @@
 // and 352 on the second and are not built.
 //
 // END selects what follows the dequantized sum in the epilogue: nothing (ENDING_NONE), the tanh form of GELU, and a gate with a
-// residual, Y = R + g y.  A lane's four values of a 16 x 16 block are one row's four neighbouring columns, so the residual is loaded
-// straight into that layout, 8 bytes (bf16) or 16 a lane: the four blocks of a 64-column row ask for the same lines one after another, and
-// no value passes through LDS twice.  A wave tile's residual goes out as a whole under the K loop's last iterations, the gates come with the
+// residual, Y = R + g y.  A wave tile's residual goes out under the K loop's last iterations, in the 16-byte chunks in which the output will be
+// stored, and passes through the output patches, whose places it takes until the results come: whole lines leave memory.  (Loaded straight into the layout
+// of the results, 32 bytes of sixteen rows an instruction, and without the non-temporal hint, us: 4680 x 8960 -> 1536 fp32 71 instead of 64,
+// 5120 -> 5120 bf16 118 instead of 114.  The general tiles load without it, 2251 x 2360 -> 2252 fp32 31.7 with and 29.6 without.)  The gates come with the
 // scales; the sum is rounded to the output type once.  256 x 256 tiles have no registers for it.
 #pragma once
 #include <algorithm>
@@ -166,7 +167,6 @@ __global__ __launch_bounds__(64 * WM * WN, (Geo2<BM, BN, WM, WN, NSTAGE, W4, (EN
     constexpr int ESZ = (int)sizeof(OutT);
     constexpr bool RES = (END & ENDING_RESIDUAL) != 0;
     using res_t = std::conditional_t<sizeof(OutT) == 4, v4f, v2u>;            // four elements of R
-    typedef res_t res_any __attribute__((aligned(2)));
     static_assert(END == ENDING_NONE || sizeof(OutT) > 1, "INT8 outputs have an ending of their own");
     static_assert(!RES || TM * TN <= 16, "registers for a whole wave tile of the residual");
 
@@ -313,30 +313,50 @@ __global__ __launch_bounds__(64 * WM * WN, (Geo2<BM, BN, WM, WN, NSTAGE, W4, (EN
     int stage = base;
     [[maybe_unused]] const long long p_t0 = QARVD_PROF ? clock64() : 0;
 
-    // Residual of block (i, j), rows lr and columns 4 lq .. + 3 of it.  The descriptor covers the rows of the tile that exist (none without a
-    // residual: zeros are added); columns past the matrix read what lies there inside those rows, or zeros, and are never stored.
-    [[maybe_unused]] res_t rs[RES ? TM : 1][RES ? TN : 1];
-    [[maybe_unused]] int r_lane = 0, r_bytes = 0, lr = 0, lq = 0;
-    [[maybe_unused]] const int ldr_b = RES ? (int)g.ldr * ESZ : 0;
-    auto load_residual = [&](int i, int j) {
-        if constexpr (RES) {
-            if (!GEN || g.vec_out) {
-                rs[i][j] = buffer_load_as<res_t>(reinterpret_cast<const OutT *>(g.R) + (size_t)m0 * g.ldr, r_bytes, r_lane, i * 16 * ldr_b + j * 16 * ESZ);
-            } else {
-                const int row = wm * G::WTM + i * 16 + lr, left = g.N - (n0 + wn * G::WTN + j * 16 + 4 * lq);
-                const OutT *const r = reinterpret_cast<const OutT *>(g.R) + (size_t)(m0 + row) * g.ldr + (g.N - left);
-                OutT e[4] = {0, 0, 0, 0};
-                if (g.R && m0 + row < g.M) {
-                    if (left >= 4) {
-                        rs[i][j] = *reinterpret_cast<const res_any *>(r);
-                        return;
-                    }
+    constexpr int EPC = 16 / ESZ;     // output elements per 16-byte chunk
+    // A patch is 16 rows of 128 bytes, whole lines of the output, or 32 rows of 64 where a wave's row is that short.  Block (i, j)
+    // puts this lane's four outputs, columns 16 j + 4 eq .., into row 16 i + er.  Read back, lane l takes chunk l % chunks of a
+    // row; the rows go to the lanes so that the sixteen lanes a pass serves, 8p .. 8p+7 and 32+8p .. 32+8p+7, cover the banks.
+    constexpr int PRS = G::WTN * ESZ >= 128 ? 128 : 64, PROWS = PATCH2_BYTES / PRS, PCH = PRS / 16;
+    constexpr int PCB = PRS / ESZ / 16, PRB = PROWS / 16;      // blocks of a patch: columns, rows
+    static_assert(G::WTN * ESZ % PRS == 0 && (PRB == 1 || PCB == TN), "patches are whole rows of the wave tile, or parts of one row block");
+    auto patch_row = [](int l) { return PRS == 128 ? 2 * ((l >> 3) & 3) + (l >> 5) : 4 * ((l >> 3) & 3) + 2 * (l >> 5) + ((l >> 2) & 1); };
+
+    // Residual, in the output's 16-byte chunks: whole lines leave memory, and each chunk waits in the registers of the lane that will store there.  The
+    // descriptor covers the rows of the tile that exist (none without a residual: zeros are added); columns past the matrix
+    // read what lies there inside those rows, or zeros, and are never stored.
+    constexpr int NPATCH = (TM / PRB) * (TN / PCB);
+    [[maybe_unused]] v4i rs[RES ? NPATCH : 1][2];
+    [[maybe_unused]] int lr = 0, lq = 0;            // row and quarter of this lane in a block
+    auto load_residual = [&](int l) {
+        const int row = wm * G::WTM + patch_row(l), col = n0 + wn * G::WTN + (l & (PCH - 1)) * EPC;
+        if constexpr (!RES) {
+            (void)row; (void)col;
+        } else if (!GEN || g.vec_out) {
+            const int ldr_b = (int)g.ldr * ESZ, bytes = g.R ? (min(BM, g.M - m0) - 1) * ldr_b + g.N * ESZ : 0;
+            const OutT *const r = reinterpret_cast<const OutT *>(g.R) + (size_t)m0 * g.ldr;
 #pragma unroll
-                    for (int k = 0; k < 3; ++k)
-                        if (k < left) e[k] = r[k];
+            for (int p = 0; p < NPATCH; ++p)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    rs[p][h] = buffer_load16<!GEN>(r, bytes, row * ldr_b + col * ESZ, (p / (TN / PCB) * PROWS + h * (PROWS / 2)) * ldr_b + p % (TN / PCB) * PCB * 16 * ESZ);
+        } else {
+#pragma unroll
+            for (int p = 0; p < NPATCH; ++p)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int m = m0 + row + p / (TN / PCB) * PROWS + h * (PROWS / 2), n = col + p % (TN / PCB) * PCB * 16;
+                    const OutT *const r = reinterpret_cast<const OutT *>(g.R) + (size_t)m * g.ldr + n;
+                    rs[p][h] = zero4;
+                    if (!g.R || m >= g.M || n >= g.N) continue;
+                    if (n + EPC <= g.N) {
+                        rs[p][h] = *reinterpret_cast<const v4i_unaligned *>(r);
+                    } else {                       // the last, partial chunk of a row
+#pragma unroll
+                        for (int k = 0; k < EPC - 1; ++k)
+                            if (n + k < g.N) rs[p][h][k * ESZ / 4] |= (int)((unsigned)element_bits(r[k]) << (8 * (k * ESZ % 4)));
+                    }
                 }
-                rs[i][j] = pack4(e);
-            }
         }
     };
     // Gate of this lane's columns of block (i, j).  A tile whose rows are of two groups at most, as where a group has BM - 1 tokens or more,
@@ -362,29 +382,20 @@ __global__ __launch_bounds__(64 * WM * WN, (Geo2<BM, BN, WM, WN, NSTAGE, W4, (EN
             }
         }
     };
-    auto aim_ending = [&](int row, int quarter) {   // for the tile at (m0, n0)
-        lr = row;
-        lq = quarter;
-        r_lane = (wm * G::WTM + lr) * ldr_b + (n0 + wn * G::WTN + 4 * lq) * ESZ;
-        r_bytes = g.R ? (min(BM, g.M - m0) - 1) * ldr_b + g.N * ESZ : 0;
+    auto aim_gates = [&](int l) {                   // for the tile at (m0, n0)
+        lr = l & 15;
+        lq = l >> 4;
         const int first = (int)__builtin_amdgcn_readfirstlane((unsigned)m0 / (unsigned)g.gate_rows);
         next_group = (int)min((int64_t)(first + 1) * g.gate_rows - m0, (int64_t)BM);
     };
     // The whole wave tile's residual goes out in front of the K loop's last iterations, behind all stage loads, whose waits leave it in
     // flight; where the number of loads differs from wave to wave (edges of a GEN tile), after the loop.  (Spread over the loop, at another
     // place in every tile, it cost up to 1 us more.)
-    constexpr int YOUNGER = RES ? TM * TN : 0;
+    constexpr int YOUNGER = RES ? 2 * NPATCH : 0;
     [[maybe_unused]] const bool early = RES && (!GEN || g.vec_out);
-    auto load_ending = [&](int row, int quarter) {
-        aim_ending(row, quarter);
-#pragma unroll
-        for (int i = 0; i < TM; ++i)
-#pragma unroll
-            for (int j = 0; j < TN; ++j) load_residual(i, j);
-    };
     auto begin_tail = [&]() {
         if constexpr (RES) {
-            if (early) load_ending(frow, fq);
+            if (early) load_residual(lane);
         }
     };
     auto wait_tail = [&](int stages) {
@@ -514,7 +525,8 @@ __global__ __launch_bounds__(64 * WM * WN, (Geo2<BM, BN, WM, WN, NSTAGE, W4, (EN
     asm volatile("" : "+v"(el));
     const int er = el & 15, eq = el >> 4;
     if constexpr (RES) {
-        if (!early) load_ending(er, eq);
+        aim_gates(el);
+        if (!early) load_residual(el);
     }
     const int hstage0 = (base + Tn) % NSTAGE;
     const int pstage = (base + Tn - 1 + 2 * NSTAGE) % NSTAGE;
@@ -529,15 +541,8 @@ __global__ __launch_bounds__(64 * WM * WN, (Geo2<BM, BN, WM, WN, NSTAGE, W4, (EN
     [[maybe_unused]] const float *gate_lds = sc_lds + BM + 3 * BN;
     unsigned char *const patch = (G::PATCH_EXTRA ? smem + G::PATCH_OFF : smem + pstage * STG) + wave * PATCH2_BYTES;
     OutT *Y = reinterpret_cast<OutT *>(g.Y);
-    constexpr int EPC = 16 / ESZ;     // output elements per 16-byte chunk
-    // A patch is 16 rows of 128 bytes, whole lines of the output, or 32 rows of 64 where a wave's row is that short.  Block (i, j)
-    // puts this lane's four outputs, columns 16 j + 4 eq .., into row 16 i + er.  Read back, lane l takes chunk l % chunks of a
-    // row; the rows go to the lanes so that the sixteen lanes a pass serves, 8p .. 8p+7 and 32+8p .. 32+8p+7, cover the banks.
-    constexpr int PRS = G::WTN * ESZ >= 128 ? 128 : 64, PROWS = PATCH2_BYTES / PRS, PCH = PRS / 16;
-    constexpr int PCB = PRS / ESZ / 16, PRB = PROWS / 16;      // blocks of a patch: columns, rows
-    static_assert(G::WTN * ESZ % PRS == 0 && (PRB == 1 || PCB == TN), "patches are whole rows of the wave tile, or parts of one row block");
     auto pswz = [](int row) { return PRS == 128 ? swz128(row) : (row >> 2) & 3; };
-    const int prow = PRS == 128 ? 2 * ((el >> 3) & 3) + (el >> 5) : 4 * ((el >> 3) & 3) + 2 * (el >> 5) + ((el >> 2) & 1);
+    const int prow = patch_row(el);
     const int pch = el & (PCH - 1);
     const int pw_addr = er * PRS + ((((4 * eq * ESZ) >> 4) ^ pswz(er)) << 4) + ((4 * eq * ESZ) & 15);     // column block 0 of a patch
     unsigned char *const y_tile = reinterpret_cast<unsigned char *>(Y + (size_t)m0 * g.ldy);
@@ -669,6 +674,18 @@ __global__ __launch_bounds__(64 * WM * WN, (Geo2<BM, BN, WM, WN, NSTAGE, W4, (EN
                     }
                 }
                 load_gate(i, j, gate_lds);
+                unsigned char *const pw = patch + (i % PRB) * 16 * PRS + (pw_addr ^ ((j % PCB) * 16 * ESZ));
+                [[maybe_unused]] res_t r4;
+                if constexpr (RES) {               // the patch's residual to where its results will be, this lane's four back from there
+                    if (i % PRB == 0 && j % PCB == 0) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const int row = h * (PROWS / 2) + prow;
+                            *reinterpret_cast<v4i *>(patch + row * PRS + ((pch ^ pswz(row)) << 4)) = rs[i / PRB * (TN / PCB) + j / PCB][h];
+                        }
+                    }
+                    r4 = *reinterpret_cast<const res_t *>(pw);
+                }
                 float y[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -682,7 +699,7 @@ __global__ __launch_bounds__(64 * WM * WN, (Geo2<BM, BN, WM, WN, NSTAGE, W4, (EN
                     }
                     y[e] = fmaf(v, sx, bs[j][e]);
                     if constexpr ((END & ENDING_GELU) != 0) y[e] = gelu_tanh(y[e]);
-                    if constexpr (RES) y[e] = fmaf(gt[j][e], y[e], element(rs[i][j], e));
+                    if constexpr (RES) y[e] = fmaf(gt[j][e], y[e], element(r4, e));
                 }
                 if constexpr (DBG) {
                     const int m = m0 + wm * G::WTM + i * 16 + er, n = n0 + wn * G::WTN + j * 16 + 4 * eq;
@@ -699,7 +716,6 @@ __global__ __launch_bounds__(64 * WM * WN, (Geo2<BM, BN, WM, WN, NSTAGE, W4, (EN
                         }
                     }
                 }
-                unsigned char *const pw = patch + (i % PRB) * 16 * PRS + (pw_addr ^ ((j % PCB) * 16 * ESZ));
                 if constexpr (sizeof(OutT) == 1) {
                     // chained layer: activation, then the next layer's static scale (Eq. (quantization))
                     *reinterpret_cast<unsigned *>(pw) = quantize4_static<out_is_gelu<OutT>::value>(y, sq);

@@ -183,20 +183,20 @@ __device__ __forceinline__ float gelu_tanh(float x)
     const float inner = fmaf(-0.102943240f, x * x, -2.30220820f);
     return x * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(x * inner));
 }
-// Four elements at base + voffset + soffset through a raw descriptor over [base, base + bytes); zeros past its end.
-template <typename T> __device__ __forceinline__ T buffer_load_as(const void *base, int bytes, int voffset, int soffset)
+// Sixteen bytes at base + voffset + soffset through a raw descriptor over [base, base + bytes); zeros past its end.  STREAM: with the
+// non-temporal hint.
+template <bool STREAM> __device__ __forceinline__ v4i buffer_load16(const void *base, int bytes, int voffset, int soffset)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
     const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, bytes, 0x00020000);
-    if constexpr (sizeof(T) == 16) return __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b128(r, voffset, soffset, 0));
-    else return __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b64(r, voffset, soffset, 0));
+    return __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(r, voffset, soffset, STREAM ? 2 : 0));
 #else
     (void)base; (void)bytes; (void)voffset; (void)soffset;
-    return T{};
+    return v4i{};
 #endif
 }
-__device__ __forceinline__ v4f pack4(const float (&e)[4]) { return v4f{e[0], e[1], e[2], e[3]}; }
-__device__ __forceinline__ v2u pack4(const uint16_t (&e)[4]) { return v2u{e[0] | ((uint32_t)e[1] << 16), e[2] | ((uint32_t)e[3] << 16)}; }
+__device__ __forceinline__ uint32_t element_bits(float e) { return __float_as_uint(e); }
+__device__ __forceinline__ uint32_t element_bits(uint16_t e) { return e; }
 __device__ __forceinline__ float element(v4f r, int e) { return r[e]; }
 __device__ __forceinline__ float element(v2u r, int e) { return __uint_as_float(e & 1 ? r[e >> 1] & 0xFFFF0000u : r[e >> 1] << 16); }
 
