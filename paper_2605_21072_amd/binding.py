@@ -484,7 +484,9 @@ def fused_gemm_num_variants() -> int:
 
 def _on_call_device(stream, *tensors):
     """A kernel runs on the current device, or the given stream's: its tensors have to be there."""
-    index = torch._C._cuda_getDevice() if stream is None else stream.device_index if hasattr(stream, "device_index") else stream.device.index
+    index = getattr(stream, "device_index", None)           # (absent where a stream is given by its handle alone)
+    if index is None:
+        index = torch._C._cuda_getDevice()
     for t in tensors:
         if t is not None and t.get_device() != index:
             raise ValueError("a tensor is on %s, the call on device %d" % (t.device, index))
@@ -553,6 +555,7 @@ def w8a8_dual_gemm_fused(Xq: torch.Tensor, s_x: torch.Tensor, w: DualScaleWeight
         _check(st, "qarvd_dual_gemm_fused")
         return Y
     dtype = out_dtype if Y is None else Y.dtype
+    _vector(bias, w.N, "bias")
     e = _ending(M, w.N, act, gate, gate_rows, residual, dtype)
     if dtype not in _DTYPES:
         raise TypeError("expected float32 or bfloat16, got %s" % dtype)
@@ -581,6 +584,7 @@ def w8a8_linear_fused(X: torch.Tensor, w: DualScaleWeight, bias: Optional[torch.
     if K != w.K:
         raise ValueError("X has %d channels, the layer %d" % (K, w.K))
     dtype = out_dtype if Y is None else Y.dtype
+    _vector(bias, w.N, "bias")
     e = _ending(M, w.N, act, gate, gate_rows, residual, dtype)
     if dtype not in _DTYPES:
         raise TypeError("expected float32 or bfloat16, got %s" % dtype)
@@ -664,6 +668,8 @@ def qk_norm_rope(Q: torch.Tensor, K: Optional[torch.Tensor], norm: int = NORM_HE
         return out_q, out_k
     _check_heads(Q, "Q")
     M, hq, D = Q.shape
+    if M > 2**31 - 1:
+        raise ValueError("more than 2^31 - 1 tokens")
     _norm_weight(weight_q, norm, hq, D, "weight_q")
     r = _rope(rope, pos, M)
     if K is None:
@@ -704,6 +710,7 @@ def w8a8_linear_qkv(X: torch.Tensor, w: DualScaleWeight, bias: Optional[torch.Te
     M, K = X.shape
     if K != w.K:
         raise ValueError("X has %d channels, the layer %d" % (K, w.K))
+    _vector(bias, w.N, "bias")
     _norm_weight(weight_q, norm, heads_q, head_dim, "weight_q")
     _norm_weight(weight_k, norm, heads_k, head_dim, "weight_k")
     r = _rope(rope, pos, M)

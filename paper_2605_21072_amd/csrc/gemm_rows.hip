@@ -248,7 +248,7 @@ __global__ __launch_bounds__(64 * NW) void gemm_rows_kernel(GemmArgs g, RowsX in
         const int m = i / COLS, c = i % COLS, n = n0 + c;
         if (m >= g.M || n >= g.N) continue;
         constexpr float ws = W4 ? 0.0625f : 1.0f;     // INT4 codes enter the matrix instructions times 16
-        float v = (float)sums[0][m][c] * (g.s_o[n] * ws);
+        float v = (float)sums[0][m][c] * (g.n_off > 0 ? g.s_o[n] * ws : 0.0f);
         v = fmaf((float)sums[1][m][c], g.s_n[n] * ws, v);
         v = fmaf(v, QUANT ? own_scale : g.s_x[m], g.bias ? g.bias[n] : 0.0f);
         if (g.act == QARVD_ACT_GELU_TANH) v = gelu_tanh(v);

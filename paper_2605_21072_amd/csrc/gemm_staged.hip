@@ -142,7 +142,7 @@ __global__ __launch_bounds__(TPB) void gemm_staged_kernel(GemmArgs g)
         const int n = n0 + wn * (BN / WN) + j * 32 + frow;
         const int nc = min(n, g.N - 1);
         const float wsc = W4 ? 0.0625f : 1.0f;
-        const float sn = g.s_n[nc] * wsc, so = g.s_o[nc] * wsc;
+        const float sn = g.s_n[nc] * wsc, so = FUSED && g.n_off == 0 ? 0.0f : g.s_o[nc] * wsc;
         const float bs = g.bias ? g.bias[nc] : 0.0f;
 #pragma unroll
         for (int i = 0; i < TM; ++i) {

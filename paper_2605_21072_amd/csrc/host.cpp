@@ -5,6 +5,8 @@
 // from the ctypes library, so that there is one copy of it.
 #include <Python.h>
 
+#include <stdint.h>
+
 #include <algorithm>
 #include <initializer_list>
 #include <string>
@@ -181,6 +183,14 @@ void check_out(const at::Tensor &t, int64_t M, int64_t N, const char *what)
         throw py::value_error(std::string(what) + " must be [M, N] with unit inner stride");
 }
 
+void check_vector(const OptTensor &t, int64_t n, const char *what)
+{
+    if (!t) return;
+    if (t->scalar_type() != at::kFloat) throw py::type_error(std::string(what) + " must be float32");
+    if (t->dim() != 1 || t->size(0) != n || (n > 1 && t->stride(0) != 1))
+        throw py::value_error(std::string(what) + " must be a contiguous vector of " + std::to_string(n));
+}
+
 qarvd_ending make_ending(int64_t M, int64_t N, int act, const OptTensor &gate, std::optional<int64_t> gate_rows, const OptTensor &residual,
                          at::ScalarType dtype)
 {
@@ -218,6 +228,7 @@ py::tuple gemm_fused(const at::Tensor &Xq, const OptTensor &s_x, int bits, const
                      int64_t device)
 {
     const at::ScalarType out = Y ? Y->scalar_type() : c10::dtype_or_default(out_dtype);
+    check_vector(bias, N, "bias");
     const qarvd_ending e = make_ending(M, N, act, gate, gate_rows, residual, out);
     const qarvd_dtype ydt = dtype_of(out);
     on_device(device, {&Xq, opt(s_x), &Wq, opt(bias), opt(gate), opt(residual), opt(Y)});
@@ -240,6 +251,7 @@ py::tuple linear_fused(const at::Tensor &X, const OptTensor &perm, int bits, con
     const int64_t M = X.size(0);
     if (X.size(1) != K) throw py::value_error("X has " + std::to_string(X.size(1)) + " channels, the layer " + std::to_string(K));
     const at::ScalarType out = Y ? Y->scalar_type() : c10::dtype_or_default(out_dtype);
+    check_vector(bias, N, "bias");
     const qarvd_ending e = make_ending(M, N, act, gate, gate_rows, residual, out);
     const qarvd_dtype xdt = dtype_of(X.scalar_type()), ydt = dtype_of(out);
     on_device(device, {&X, &Wq, opt(bias), opt(gate), opt(residual), opt(Y)});
@@ -284,12 +296,8 @@ bool make_rope(const std::optional<std::vector<int64_t>> &axes, const OptTensor 
 
 void check_norm_weight(const OptTensor &w, int norm, int64_t heads, int64_t D, const char *what)
 {
-    if (!w) return;
-    if (norm == QARVD_NORM_NONE) throw py::value_error(std::string(what) + " without a norm");
-    if (w->scalar_type() != at::kFloat) throw py::type_error(std::string(what) + " must be float32");
-    const int64_t n = norm == QARVD_NORM_ROW ? heads * D : D;
-    if (w->dim() != 1 || w->size(0) != n || (n > 1 && w->stride(0) != 1))
-        throw py::value_error(std::string(what) + " must be a contiguous vector of " + std::to_string(n));
+    if (w && norm == QARVD_NORM_NONE) throw py::value_error(std::string(what) + " without a norm");
+    check_vector(w, norm == QARVD_NORM_ROW ? heads * D : D, what);
 }
 
 void check_heads(const at::Tensor &x, const char *what, const at::Tensor *like = nullptr)
@@ -311,6 +319,7 @@ py::tuple heads(const at::Tensor &Q, const OptTensor &K, int norm, const OptTens
 {
     check_heads(Q, "Q");
     const int64_t M = Q.size(0), D = Q.size(2);
+    if (M > INT32_MAX) throw py::value_error("more than 2^31 - 1 tokens");
     check_norm_weight(wq, norm, Q.size(1), D, "weight_q");
     qarvd_rope r;
     const bool turn = make_rope(axes, freq, interleaved, pos, M, &r);
@@ -345,6 +354,7 @@ py::tuple linear_qkv(const at::Tensor &X, const OptTensor &perm, int bits, const
     check_2d(X, "X");
     const int64_t M = X.size(0);
     if (X.size(1) != K) throw py::value_error("X has " + std::to_string(X.size(1)) + " channels, the layer " + std::to_string(K));
+    check_vector(bias, N, "bias");
     check_norm_weight(wq, norm, heads_q, D, "weight_q");
     check_norm_weight(wk, norm, heads_k, D, "weight_k");
     qarvd_rope r;

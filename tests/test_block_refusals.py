@@ -1,5 +1,6 @@
 """What the fused endings and the head norms refuse, on the host and before anything is launched: no GPU needed."""
 import ctypes as C
+import types
 
 import pytest
 import torch
@@ -103,6 +104,9 @@ def bad_endings(put):
                      (dict(Y=b[:2]), ValueError), (dict(Y=z(N, M).t()), ValueError), (dict(out_dtype=torch.float16), TypeError)):
         yield lambda s, bad=bad: q.w8a8_linear_fused(X, w, None, stream=s, **bad), err
         yield lambda s, bad=bad: q.w8a8_dual_gemm_fused(Xq, put(torch.ones(M)), w, None, M, stream=s, **bad), err
+    for bias, err in ((z(N, dtype=torch.bfloat16), TypeError), (z(N - 1), ValueError), (z(N, 2)[:, 0], ValueError)):
+        yield lambda s, bias=bias: q.w8a8_linear_fused(X, w, bias, stream=s), err
+        yield lambda s, bias=bias: q.w8a8_dual_gemm_fused(Xq, put(torch.ones(M)), w, bias, M, stream=s), err
     yield lambda s: q.w8a8_linear_fused(put(torch.zeros(M, K - 1)), w, None, stream=s), ValueError
     yield lambda s: q.w8a8_linear_fused(torch.zeros(M, K), w, None, stream=s), ValueError              # not on the device
     yield lambda s: q.w8a8_dual_gemm_fused(Xq, put(torch.ones(9)), w, None, M + 1, stream=s), ValueError
@@ -170,6 +174,8 @@ def test_tensors_of_another_device_are_refused(lib, monkeypatch):
     binding._on_call_device(None, On(1), None, On(1))
     with pytest.raises(ValueError):
         binding._on_call_device(None, On(1), On(0))
+
+    binding._on_call_device(types.SimpleNamespace(cuda_stream=0), On(1))        # a stream that is a handle: the current device
 
     class Stream:
         device_index = 0

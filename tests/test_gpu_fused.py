@@ -68,7 +68,8 @@ def inputs(seed, M, K, N, dtype, act, gates, residual):
 ENDINGS = [(1, 0, False), (0, 0, True), (0, 3, True), (1, 2, True), (0, 1, False), (1, 1, False), (0, 0, False)]     # act, gate rows, residual
 #        M, N, K, K_o: one token; whole tiles; ragged rows; more tiles than CUs; any N; wide and odd outlier blocks; short K
 SHAPES = [(1, 64, 128, 0), (256, 256, 256, 32), (300, 520, 1000, 96), (129, 1544, 384, 128), (2100, 1536, 256, 64), (77, 131, 200, 7),
-          (70, 264, 640, 200), (1, 1, 1, 0), (17, 8, 96, 96), (65, 24, 33, 33)]
+          (70, 264, 640, 200), (1, 1, 1, 0), (17, 8, 96, 96), (65, 24, 33, 33),
+          (140, 516, 256, 32), (1, 40, 5000, 0)]
 
 
 @pytest.mark.parametrize("bits", [8, 4])
@@ -236,6 +237,26 @@ def test_infinities_and_nan_stay_where_they_are(N):
     X[7] = 0.0                                   # a token of zeros: its scale is 0, what is left is the bias
     Y = q.w8a8_linear_fused(X, w, bias, act=1, out_dtype=torch.float32)
     check(Y[7:8], bias.cpu().double().unsqueeze(0), torch.zeros((1, N), dtype=torch.float64), 1, None, None, None)
+
+
+def test_without_outliers_their_scales_are_not_read():
+    """No outlier block: what stands in s_outlier is of no matter, on any kernel."""
+    for bits in (8, 4):
+        for N, K in ((520, 256), (131, 300)):
+            w, _ = layer(21, N, K, 0, bits)
+            for M in (1, 5, 20, 300):
+                X, bias, gate, R = inputs(22, M, K, N, torch.float32, 0, 1, True)
+                want = q.w8a8_linear_fused(X, w, bias, gate=gate, residual=R, out_dtype=torch.float32)
+                keep, w.s_outlier = w.s_outlier, torch.full_like(w.s_outlier, float("nan"))
+                Xq, s_x = q.quant_act(X, None, 0)
+                for v in range(q.fused_gemm_num_variants() + 1):
+                    try:
+                        got = q.w8a8_dual_gemm_fused(Xq, s_x, w, bias, M, gate=gate, residual=R, out_dtype=torch.float32, variant=v)
+                    except q.QarvdError:
+                        continue
+                    assert torch.equal(got, want), v
+                assert torch.equal(q.w8a8_linear_fused(X, w, bias, gate=gate, residual=R, out_dtype=torch.float32), want)
+                w.s_outlier = keep
 
 
 def test_gelu_far_from_zero():
