@@ -137,22 +137,40 @@ def test_few_rows(N, K, K_o, bits):
 
 
 @pytest.mark.parametrize("bits", [8, 4])
-@pytest.mark.parametrize("K,K_o", [(4, 0), (3, 3), (97, 33), (1536, 32), (8960, 64), (10240, 0), (10239, 160), (10240, 10240), (10241, 32)])
-def test_one_token_quantized_on_the_way(K, K_o, bits):
-    """One row is quantized by the GEMM's own workgroups up to 10240 channels: the codes and the scale of quant_act, whatever the row's size."""
+@pytest.mark.parametrize("K,K_o", [(4, 0), (3, 3), (97, 33), (1536, 32), (2048, 1), (2047, 2047), (2048, 0), (2049, 64), (8960, 64), (10240, 0), (10239, 160),
+                                   (10240, 10240), (10241, 32)])
+def test_tokens_quantized_on_the_way(K, K_o, bits):
+    """One row is quantized by the GEMM's own workgroups, up to 10240 channels: the codes and scales of quant_act, whatever the rows' sizes."""
     N = 72
     w, _ = layer(K, N, K, K_o, bits)
     gen = torch.Generator(device="cuda").manual_seed(K)
+    scales = torch.tensor([1.0, 0.0, 1e-36, 3e34, 1e-30, 1.0, 1e-4, 1e4, 1.0, 0.0, 1.0, 1e-36, 1.0, 1.0, 3e34, 1.0, 1.0], device="cuda")
     for dtype in (torch.float32, torch.bfloat16):
-        row = torch.randn((1, K + 1), generator=gen, device="cuda")
-        row[0, ::7] *= 15
-        for scale in (1.0, 0.0, 1e-36, 1e-30, 3e34, float("inf")):
-            X = (row * scale if scale < 1e38 else row.masked_fill(row > 3, scale)).to(dtype)[:, 1:]       # (an odd address, too)
-            Xq, s_x = q.quant_act(X, w.perm if K_o else None, K_o)
-            bias, R = torch.randn(N, generator=gen, device="cuda"), torch.randn((1, N), generator=gen, device="cuda")
-            want = q.w8a8_dual_gemm_fused(Xq, s_x, w, bias, 1, residual=R, out_dtype=torch.float32)
-            got = q.w8a8_linear_fused(X, w, bias, residual=R, out_dtype=torch.float32)
-            assert torch.equal(got.view(torch.int32), want.view(torch.int32)), (dtype, scale)
+        for M in (1, 2, 7, 8, 9, 16, 17):
+            rows = torch.randn((M, K + 1), generator=gen, device="cuda")
+            rows[:, ::7] *= 15
+            for first in range(5 if M == 1 else 1):
+                X = rows * scales[first:first + M, None]
+                if M != 2:
+                    X[M - 1] = torch.where(rows[M - 1] > 3, float("inf"), X[M - 1]) if first == 0 and M > 2 else X[M - 1]
+                X = X.to(dtype)[:, 1:]                   # (an odd address, too)
+                Xq, s_x = q.quant_act(X, w.perm if K_o else None, K_o)
+                bias, R = torch.randn(N, generator=gen, device="cuda"), torch.randn((M, N), generator=gen, device="cuda")
+                want = q.w8a8_dual_gemm_fused(Xq, s_x, w, bias, M, residual=R, out_dtype=torch.float32)
+                got = q.w8a8_linear_fused(X, w, bias, residual=R, out_dtype=torch.float32)
+                assert torch.equal(got.view(torch.int32), want.view(torch.int32)), (dtype, M, first)
+
+
+@pytest.mark.parametrize("N", [2048, 2056, 4096, 4104])
+def test_tokens_quantized_on_the_way_by_width(N):
+    """Outputs on either side of what one round of workgroups holds."""
+    K, K_o = 520, 40
+    w, _ = layer(N, N, K, K_o, 8)
+    for M in (1, 8, 9, 16):
+        X, bias, gate, R = inputs(M, M, K, N, torch.bfloat16, 1, 1, True)
+        Xq, s_x = q.quant_act(X, w.perm, K_o)
+        want = q.w8a8_dual_gemm_fused(Xq, s_x, w, bias, M, act=1, gate=gate, residual=R)
+        assert torch.equal(q.w8a8_linear_fused(X, w, bias, act=1, gate=gate, residual=R), want)
 
 
 @pytest.mark.parametrize("M,rows", [(300, 1), (300, 7), (300, 100), (300, 255), (300, 256), (300, 299), (1100, 300), (1100, 520), (40, 40), (40, 1 << 30)])
