@@ -64,8 +64,9 @@ __device__ __forceinline__ float wave_sum(float v)
     return v;
 }
 
-// Any head size, stride and alignment: a workgroup has a token's queries or its keys, a wave every fourth head, and the elements
-// are loaded one by one, a second time after the norm is known (the caches hold them).
+// What the kernel below has no room for: rows of more than 64 vectors under one norm, heads of more than 64 lanes (512 channels of which a part turns
+// in halves).  A workgroup has a token's queries or its keys, a wave every fourth head, and the elements are loaded one by one, a second time after
+// the norm is known (the caches hold them).
 template <typename T>
 __global__ __launch_bounds__(TPB) void heads_any_kernel(HeadArgs a)
 {
@@ -120,7 +121,9 @@ __global__ __launch_bounds__(TPB) void heads_any_kernel(HeadArgs a)
 // to a head, whole heads side by side.  All loads go out first, then lane i works out the angle of pair i, once for the
 // token instead of once in every lane that needs it, and the wave reads them back from LDS in the order of its channels: a lane's four pairs
 // are the same in every vector, so they stay in registers, like a head's weights.
-//   interleaved  the lane's channels are 8 j .. 8 j + 7, its pairs 4 j .. 4 j + 3
+//   interleaved  bf16: the lane's channels are 8 j .. 8 j + 7, its pairs 4 j .. 4 j + 3
+//                fp32: channels 4 j .. and D/2 + 4 j .., so that neighbouring lanes' 16-byte pieces are neighbours in memory: 24 heads of 128
+//                with a row's norm, 1560 tokens 12.9 -> 8.3 us, 4680 37.5 -> 22.7
 //   HALF         channels 4 j .. and R/2 + 4 j .., the same pairs; lanes behind the rotary channels have 8 neighbours again
 // WHOLE: every lane's pieces are whole and 16-byte aligned (HALF bf16: 8).  Otherwise they are loaded from any address, and the last lane of a
 // head (HALF: also of its rotary channels) takes what there is one by one.
@@ -128,6 +131,7 @@ struct FastArgs {
     HeadArgs h;
     int32_t lph_log, hpv_log;      // lanes to a head, heads to a vector (log2)
     int32_t rotary_lanes;          // (HALF) lanes of a head that hold pairs
+    int32_t lanes;                 // lanes of a head that hold channels
     int32_t nv[2], parts_q;        // vectors of a token's queries and keys; how many waves share the queries
     int32_t write_through;         // how the outputs leave (see stores_through)
     float inv_n[2];                // 1 / (channels under a norm)
@@ -210,26 +214,37 @@ template <int CH> __device__ __forceinline__ void group_sum(float (&v)[CH], int 
     if (log > 5) all([](int x) { return __shfl_xor(x, 32, 64); });
 }
 
-template <typename T, int CH, bool HALF, int NORM, bool WHOLE>
-__global__ __launch_bounds__(TPB) void heads_kernel(FastArgs f)
+// SPLIT (the norm of a row of several waves): a workgroup has one token's queries or its keys; its waves share the angles and add up their sums.
+// Against one wave that holds the whole row, us for 80 heads of 128 bf16: one token 7.2 -> 3.4, 1560 18.0 -> 13.4, 4680 53.5 -> 44.7.
+constexpr int MOST_WAVES = 16, MOST_VECTORS = 64;
+template <typename T, int CH, bool HALF, int NORM, bool WHOLE, bool SPLIT>
+__global__ __launch_bounds__(SPLIT ? 64 * MOST_WAVES : TPB) void heads_kernel(FastArgs f)
 {
     typedef typename Four<T>::raw raw;
     constexpr bool WIDE = WHOLE && !HALF && sizeof(T) == 2;         // the eight channels are one 16-byte piece
-    __shared__ __align__(16) float turns[TPB / 64][MAX_D];
+    constexpr bool APART = !HALF && sizeof(T) == 4;
+    __shared__ __align__(16) float turns[SPLIT ? 1 : TPB / 64][MAX_D];
+    __shared__ float red[SPLIT ? MOST_VECTORS : 1];
     const HeadArgs &a = f.h;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int m = blockIdx.x * (TPB / 64) + wave;
+    const int m = SPLIT ? blockIdx.x : blockIdx.x * (TPB / 64) + wave;
     if (m >= a.M) return;
     const bool keys = (int)blockIdx.y >= f.parts_q;
     const Tensor &t = a.t[keys];
-    const int first = ((int)blockIdx.y - (keys ? f.parts_q : 0)) * CH;     // vector
+    const int first = (SPLIT ? wave : (int)blockIdx.y - (keys ? f.parts_q : 0)) * CH;     // vector
     const int j = lane & ((1 << f.lph_log) - 1), sub = lane >> f.lph_log;
     const bool rotary = 4 * j < a.pairs;
     const int rest = HALF ? 2 * a.pairs + 8 * (j - f.rotary_lanes) : 8 * j;       // first channel of a lane with eight neighbours
-    const int c0 = HALF && rotary ? 4 * j : rest, apart = HALF && rotary ? a.pairs : 4;
+    const int c0 = APART || (HALF && rotary) ? 4 * j : rest, apart = APART ? 4 * f.lanes : HALF && rotary ? a.pairs : 4;
     auto some = [](int left) { return min(max(left, 0), 4); };
-    const int n0 = HALF && rotary ? some(a.pairs - 4 * j) : some(a.D - rest), n1 = HALF && rotary ? n0 : some(a.D - rest - 4);
+    int n0 = some(a.D - rest), n1 = some(a.D - rest - 4);
+    if (HALF && rotary) n0 = n1 = some(a.pairs - 4 * j);
+    if (APART) {
+        n0 = some(min(a.D, apart) - c0);
+        n1 = some(a.D - apart - c0);
+    }
     const bool inside = n0 > 0;
+    auto pair = [&](int k) { return APART ? 2 * j + (k & 1) + (k & 2) * f.lanes : 4 * j + k; };       // of the lane's four
 
     const T *x = reinterpret_cast<const T *>(t.x) + (size_t)m * t.ld + c0;
     raw v[CH][2];
@@ -264,19 +279,14 @@ __global__ __launch_bounds__(TPB) void heads_kernel(FastArgs f)
     for (int k = 0; k < 8; ++k) w[k] = 1.0f;
     if (NORM == QARVD_NORM_HEAD && t.w && inside) load_weights(t.w + c0);
 
-    float co[4], si[4];
+    float *const mine = turns[SPLIT ? 0 : wave];
     if (a.pairs) {
-        float *const mine = turns[wave];
         const int32_t *pos = a.pos + (size_t)m * a.ldpos;
-        for (int i = lane; i < a.pairs; i += 64) {
+        for (int i = SPLIT ? threadIdx.x : lane; i < a.pairs; i += SPLIT ? blockDim.x : 64) {
             const float2 cs = cos_sin(pos[axis_of(a, i)], a.freq[i]);
             mine[i] = cs.x;
             mine[MAX_D / 2 + i] = cs.y;
         }
-        __builtin_amdgcn_wave_barrier();                   // (one wave's LDS accesses complete in order)
-        const v4 c4 = *reinterpret_cast<const v4 *>(mine + 4 * j), s4 = *reinterpret_cast<const v4 *>(mine + MAX_D / 2 + 4 * j);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) { co[k] = c4[k]; si[k] = s4[k]; }
     }
 
     float scale[CH];
@@ -291,10 +301,21 @@ __global__ __launch_bounds__(TPB) void heads_kernel(FastArgs f)
             }
         }
         if constexpr (NORM == QARVD_NORM_ROW) {
-#pragma unroll
-            for (int c = 1; c < CH; ++c) scale[0] += scale[c];
+            // a sum for each vector, and those in an order of their numbers: the same bits however many tokens there are and waves share the row
+            group_sum<CH>(scale, 6);
             float sum[1] = {scale[0]};
-            group_sum<1>(sum, 6);
+            if constexpr (SPLIT) {
+#pragma unroll
+                for (int c = 0; c < CH; ++c)
+                    if (lane == 0) red[first + c] = scale[c];
+                __syncthreads();
+                sum[0] = lane < CH * ((int)blockDim.x >> 6) ? red[lane] : 0.0f;
+                group_sum<1>(sum, 6);
+            } else if constexpr (CH > 1) {
+                sum[0] += scale[1];
+                if constexpr (CH == 3) sum[0] += scale[2];
+                if constexpr (CH == 4) sum[0] += scale[2] + scale[3];
+            }
 #pragma unroll
             for (int c = 0; c < CH; ++c) scale[c] = sum[0];
         } else {
@@ -302,6 +323,16 @@ __global__ __launch_bounds__(TPB) void heads_kernel(FastArgs f)
         }
 #pragma unroll
         for (int c = 0; c < CH; ++c) scale[c] = rsqrtf(fmaf(scale[c], f.inv_n[keys], a.eps));
+    }
+
+    float co[4], si[4];
+    if (a.pairs) {
+        if (!SPLIT) __builtin_amdgcn_wave_barrier();       // (one wave's LDS accesses complete in order)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            co[k] = mine[pair(k)];
+            si[k] = mine[MAX_D / 2 + pair(k)];
+        }
     }
 
     T *const out = reinterpret_cast<T *>(t.out) + (size_t)m * t.ld_out;
@@ -323,7 +354,7 @@ __global__ __launch_bounds__(TPB) void heads_kernel(FastArgs f)
                 const int p = HALF ? k : 2 * k, q = HALF ? 4 + k : 2 * k + 1;
                 const float u = e[p], z = e[q];
                 const float up = fmaf(u, co[k], -(z * si[k])), zp = fmaf(u, si[k], z * co[k]);
-                const bool turn = 4 * j + k < a.pairs;     // (selected, not multiplied by 1 and 0: the rest may be infinite)
+                const bool turn = pair(k) < a.pairs;     // (selected, not multiplied by 1 and 0: the rest may be infinite)
                 e[p] = turn ? up : u;
                 e[q] = turn ? zp : z;
             }
@@ -355,28 +386,25 @@ int ceil_log2(int n)
     return l;
 }
 
-template <typename T, bool HALF, int NORM, bool WHOLE> bool launch_fast(const FastArgs &f, int ch, int parts, hipStream_t st)
+template <typename T, bool HALF, int NORM, bool WHOLE> void launch_fast(const FastArgs &f, int ch, int waves, hipStream_t st)
 {
-    const dim3 grid((f.h.M + TPB / 64 - 1) / (TPB / 64), parts);
     auto go = [&](auto n) {
-        hipLaunchKernelGGL((heads_kernel<T, decltype(n)::value, HALF, NORM, WHOLE>), grid, dim3(TPB), 0, st, f);
-        return true;
+        constexpr int CH = decltype(n)::value;
+        if constexpr (NORM == QARVD_NORM_ROW)
+            if (waves > 1) {
+                hipLaunchKernelGGL((heads_kernel<T, CH, HALF, NORM, WHOLE, true>), dim3(f.h.M, f.nv[1] ? 2 : 1), dim3(64 * waves), 0, st, f);
+                return;
+            }
+        const dim3 grid((f.h.M + TPB / 64 - 1) / (TPB / 64), f.parts_q + (f.nv[1] + ch - 1) / ch);
+        hipLaunchKernelGGL((heads_kernel<T, CH, HALF, NORM, WHOLE, false>), grid, dim3(TPB), 0, st, f);
     };
     switch (ch) {
     case 1: return go(std::integral_constant<int, 1>{});
     case 2: return go(std::integral_constant<int, 2>{});
     case 3: return go(std::integral_constant<int, 3>{});
-    case 4: return go(std::integral_constant<int, 4>{});
-    case 5: return go(std::integral_constant<int, 5>{});
-    case 6: return go(std::integral_constant<int, 6>{});
-    case 8: return go(std::integral_constant<int, 8>{});
-    case 10: return go(std::integral_constant<int, 10>{});
-    case 16: return go(std::integral_constant<int, 16>{});
+    default: return go(std::integral_constant<int, 4>{});
     }
-    return false;
 }
-// The vectors a wave gets at least `ch` of, rounded up to a kernel that is built.
-int built(int ch) { return ch <= 6 ? ch : ch <= 8 ? 8 : ch <= 10 ? 10 : ch <= 16 ? 16 : 0; }
 
 // Vectors to a wave: as few as leave every SIMD some waves, since a wave works out its token's angles whatever it has, and at most four.  us for 1, 2, 3, 4
 // and 6: 4680 x 24 heads of 128 bf16 14.3, 13.9, 12.3, 12.3, 12.3; 1560 x 24 5.97, 5.60, 5.60, 5.63, 5.66; 520 x 80 fp32 8.98, 8.77, 8.73, 9.05, 9.47;
@@ -411,35 +439,33 @@ template <typename T> qarvd_status launch(const HeadArgs &a, hipStream_t st)
     FastArgs f;
     f.h = a;
     f.rotary_lanes = half ? (a.pairs + 3) / 4 : 0;
-    const int lanes = f.rotary_lanes + ((half ? a.D - 2 * a.pairs : a.D) + 7) / 8;
-    if (lanes <= 64) {
-        f.lph_log = ceil_log2(lanes);
+    f.lanes = f.rotary_lanes + ((half ? a.D - 2 * a.pairs : a.D) + 7) / 8;
+    if (f.lanes <= 64) {
+        f.lph_log = ceil_log2(f.lanes);
         f.hpv_log = 6 - f.lph_log;
         for (int i = 0; i < 2; ++i) {
             f.nv[i] = (a.t[i].heads + (1 << f.hpv_log) - 1) >> f.hpv_log;
             f.inv_n[i] = 1.0f / (float)(a.norm == QARVD_NORM_ROW ? (int64_t)a.t[i].heads * a.D : (int64_t)a.D);
         }
         const int most = f.nv[0] > f.nv[1] ? f.nv[0] : f.nv[1];
-        int ch = most;                       // a row's norm: one wave for all of it
-        if (a.norm != QARVD_NORM_ROW) {
-            const int64_t vectors = (int64_t)a.M * (f.nv[0] + f.nv[1]);
-            const int want = vectors >= 4 * WAVES ? 4 : vectors >= 2 * WAVES ? (int)(vectors / WAVES) : 1;
-            const int waves = (most + want - 1) / want;
-            ch = (most + waves - 1) / waves;       // evenly
-        }
+        const int64_t vectors = (int64_t)a.M * (f.nv[0] + f.nv[1]);
+        const int want = vectors >= 4 * WAVES ? 4 : vectors >= 2 * WAVES ? (int)(vectors / WAVES) : 1;
+        const bool row = a.norm == QARVD_NORM_ROW;
+        int waves = (most + want - 1) / want;
+        if (row && waves > MOST_WAVES) waves = (most + 3) / 4;
+        const int ch = (most + waves - 1) / waves;       // evenly
         f.write_through = stores_through(a, sizeof(T));
-        ch = built(ch);
-        if (ch > 0) {
-            f.parts_q = (f.nv[0] + ch - 1) / ch;
-            const int parts = f.parts_q + (f.nv[1] + ch - 1) / ch;
+        if (!row || waves <= MOST_WAVES) {
+            f.parts_q = row ? 1 : (f.nv[0] + ch - 1) / ch;
             auto as = [&](auto norm) {
                 constexpr int N = decltype(norm)::value;
-                if (whole) return half ? launch_fast<T, true, N, true>(f, ch, parts, st) : launch_fast<T, false, N, true>(f, ch, parts, st);
-                return half ? launch_fast<T, true, N, false>(f, ch, parts, st) : launch_fast<T, false, N, false>(f, ch, parts, st);
+                if (whole) return half ? launch_fast<T, true, N, true>(f, ch, waves, st) : launch_fast<T, false, N, true>(f, ch, waves, st);
+                return half ? launch_fast<T, true, N, false>(f, ch, waves, st) : launch_fast<T, false, N, false>(f, ch, waves, st);
             };
-            const bool ran = a.norm == QARVD_NORM_NONE ? as(std::integral_constant<int, QARVD_NORM_NONE>{})
-                             : a.norm == QARVD_NORM_HEAD ? as(std::integral_constant<int, QARVD_NORM_HEAD>{}) : as(std::integral_constant<int, QARVD_NORM_ROW>{});
-            if (ran) return qarvd_launch_status();
+            if (a.norm == QARVD_NORM_NONE) as(std::integral_constant<int, QARVD_NORM_NONE>{});
+            else if (row) as(std::integral_constant<int, QARVD_NORM_ROW>{});
+            else as(std::integral_constant<int, QARVD_NORM_HEAD>{});
+            return qarvd_launch_status();
         }
     }
     hipLaunchKernelGGL((heads_any_kernel<T>), dim3(a.M, a.t[1].heads > 0 ? 2 : 1), dim3(TPB), 0, st, a);

@@ -61,7 +61,8 @@ NORMS = [q.NORM_NONE, q.NORM_HEAD, q.NORM_ROW]
 SHAPES = [(1, 12, 12, 128, (44, 42, 42)), (37, 12, 12, 128, (44, 42, 42)), (5, 40, 8, 128, (128,)), (300, 3, 1, 64, (32, 32)), (9, 16, 16, 80, (40, 40)),
           (11, 10, 3, 100, (20, 22, 18)), (3, 2, 2, 512, (256, 128, 128)), (7, 5, 5, 8, (4, 2, 2)), (4, 1, 1, 2, (2,)), (6, 3, 2, 33, (16, 16)),
           (2, 2, 1, 1, ()), (13, 7, 7, 96, ()), (33, 4, 4, 72, (24, 24, 24)), (8, 6, 6, 256, (64,)), (1, 1, 1, 128, (16, 56, 56)), (21, 9, 2, 24, (8, 8)),
-          (2, 72, 72, 128, (44, 42, 42)), (6, 33, 5, 104, (52, 52))]
+          (2, 72, 72, 128, (44, 42, 42)), (6, 33, 5, 104, (52, 52)), (2, 260, 3, 128, (44, 42, 42)), (3, 2, 2, 511, (20,)), (5, 50, 50, 256, (64, 96, 96)),
+          (3, 64, 64, 512, (512,)), (500, 40, 8, 128, (44, 42, 42)), (1100, 40, 20, 100, (20, 22, 18))]
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
@@ -111,6 +112,19 @@ def test_orders_strides_and_alignment(D, axes, dtype):
             table = torch.zeros((M, 5), dtype=torch.int32, device="cuda")
             table[:, 1:1 + len(axes)] = pos
             held(q.qk_norm_rope(odd, K, norm, wq, wk, 1e-6, table[:, 1:1 + len(axes)], rope))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("hq,D", [(4, 128), (12, 128), (40, 128), (33, 100), (50, 256)])
+def test_a_token_has_the_same_bits_in_any_batch(hq, D, dtype):
+    """However many waves share a row, and however many tokens there are."""
+    M = 4700
+    for norm in NORMS:
+        _, Q, _, wq, _, pos, rope = make(norm, M, hq, hq, D, dtype, (20, 22, 18), norm, True)
+        whole, _ = q.qk_norm_rope(Q, None, norm, wq, None, 1e-6, pos, rope)
+        for first, n in ((0, 1), (3, 40), (7, 300), (20, 1500), (0, 3000)):
+            part, _ = q.qk_norm_rope(Q[first:first + n], None, norm, wq, None, 1e-6, pos[first:first + n], rope)
+            assert torch.equal(part, whole[first:first + n]), (norm, first, n)
 
 
 @pytest.mark.parametrize("far", [100_000, 30_000_000, 2**31 - 3000, -2**31 + 100])
