@@ -305,8 +305,9 @@ int32_t qarvd_q8_gemm_num_variants(void);
  *              gate_rows = its tokens); the last group may be shorter.  gate_rows >= 1; gate_rows >= M: one row, ldg is ignored
  *   residual   in  [M, ldr] of Y's type or NULL.  It may be Y itself (same address and stride): every element is read before it
  *              is written.  Any other overlap of Y with an input is undefined
- * The fastest kernels need what they need of Y, and a 16-byte aligned gate with ldg % 4 == 0, a residual aligned to four of its
- * elements with ldr % 4 == 0, ldg and ldr of at most 2^20; anything else runs on general tiles.
+ * The fastest kernels need what they need of Y (an fp32 one only N % 4 == 0), a 16-byte aligned gate with ldg % 4 == 0, at most two groups of
+ * tokens or groups of at least 63 (the larger tiles 127, 255), and a residual aligned to four of its elements with ldr % 4 == 0; ldg and ldr of at
+ * most 2^20.  Anything else runs on general tiles.
  */
 typedef struct {
     qarvd_act act;
@@ -351,7 +352,8 @@ qarvd_status qarvd_linear_fused(const void *X, qarvd_dtype xdt, int64_t ldx, con
  *   rope         HOST struct, NULL = no rotation.  pos i32 [M, ldpos] on the device, n_axes columns (1 to 3); freq f64 [R/2] on the
  *                device, radians per unit of position; axis_dims even and positive, R <= D
  * D <= 512.  Tensors aligned to their elements; the fastest kernel needs D % 8 == 0, 16-byte aligned tensors and strides that are
- * multiples of 16 bytes (and R % 8 == 0 unless interleaved).  Fully asynchronous on `stream`.
+ * multiples of 16 bytes (and R % 8 == 0 unless interleaved).  A token's result does not depend on the other tokens of the call.  Fully
+ * asynchronous on `stream`.
  */
 typedef enum { QARVD_NORM_NONE = 0, QARVD_NORM_HEAD = 1, QARVD_NORM_ROW = 2 } qarvd_norm;
 typedef struct {

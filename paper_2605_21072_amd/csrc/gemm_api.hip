@@ -76,7 +76,7 @@ bool variant_fits(const Variant &v, const GemmArgs &g, qarvd_dtype ydt)
 //     time ~ c + ceil(tiles / CUs) * (a + b * T),     T = packed K / 64          (constants in microseconds)
 // c is launch plus the first tile's lead-in, a a tile's epilogue and hand-over, b one 64-byte K step of a tile
 // that has its CU to itself (two workgroups sharing a CU each run at half speed, which the ceil over
-// the CUs already accounts for).  All tiles run on 128-byte-deep stages (gemm_dma128.hip):
+// the CUs already accounts for).  All tiles run on 128-byte-deep stages (gemm_dma128.h):
 // 256x256 has the cheapest K step per MAC and wins when N is wide; the half tiles fill the chip when N = 1536
 // (4680 x 8960 -> 1536: 54 us against 79 us for 256x256) and on M of a few hundred rows with N = 8960; 128x128
 // when those leave CUs empty (1560 x 8960 -> 1536: 29 us against 45, 1560 x 1536 -> 1536 9.4 against 13.0); 64x128 between that and

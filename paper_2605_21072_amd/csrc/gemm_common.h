@@ -14,7 +14,7 @@
 //
 // Because K_o is a multiple of 32 after padding, every 32-byte k-step lies wholly in one of the
 // two ranges: steps below the normal offset accumulate into acc_o, the rest into acc_n.
-// (gemm_dma128.hip and gemm_mfma16.hip run v_mfma_i32_16x16x64_i8: 16 rows x 64 bytes a step, which may hold the end of one range
+// (gemm_dma128.h and gemm_mfma16.hip run v_mfma_i32_16x16x64_i8: 16 rows x 64 bytes a step, which may hold the end of one range
 // and the start of the other; they say how they part it.)
 #pragma once
 #include "qarvd_common.h"
@@ -103,7 +103,7 @@ template <int BM, int BN, int WM, int WN, int NSTAGE, bool DUAL>   // INT8 outpu
 qarvd_status launch_dma_q8(const GemmArgs &g, hipStream_t st);
 template <int BM, int BN, int WM, int WN, int NSTAGE, bool DUAL>
 qarvd_status launch_dma128_q8(const GemmArgs &g, hipStream_t st);
-// 128-byte-deep K stages (gemm_dma128.hip); GEN: two accumulator sets, any outlier width, any N and output alignment
+// 128-byte-deep K stages (gemm_dma128.h); GEN: two accumulator sets, any outlier width, any N and output alignment
 template <int BM, int BN, int WM, int WN, int NSTAGE, bool DUAL, bool GEN = false, bool W4 = false>
 qarvd_status launch_dma128(const GemmArgs &g, qarvd_dtype ydt, hipStream_t st);
 // fused endings (gemm_fused.hip): g.act, g.gate, g.R

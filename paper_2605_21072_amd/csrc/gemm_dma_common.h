@@ -83,7 +83,7 @@ __device__ __forceinline__ void buffer_load_lds16(const void *base, int voffset,
 // L2: a kernel ends with a write-back of what its XCDs' L2s still hold, which for an output of a few MB is
 // most of it -- 1-2 us at the end of a 17 us GEMM.  For outputs much larger than the L2s it depends on the stores: in the kernels on
 // 64-byte stages, whose patches are half lines, it only adds traffic (4680 x 1536 bf16 18.0 -> 16.2 us, 4680 x 8960 72 -> 75); in
-// gemm_dma128.hip on whether rows begin at whole sectors (output_writes_through).
+// gemm_dma128.h on whether rows begin at whole sectors (output_writes_through).
 __device__ __forceinline__ void buffer_store16(void *base, int bytes, int voffset, int soffset, v4i data, bool write_through = false)
 {
 #if defined(__HIP_DEVICE_COMPILE__) && QARVD_NO_STORE != 2
