@@ -1,6 +1,7 @@
 // Norm of queries and keys and their rotation by position (time, height, width), one pass over both.
 //
 //     r = 1 / sqrt(mean(x^2) + eps);   x <- x r w;   (a, b) <- (a cos t - b sin t, a sin t + b cos t),   t = pos[axis(i)] freq[i]
+#include <algorithm>
 #include <type_traits>
 
 #include "qarvd_common.h"
@@ -133,6 +134,8 @@ struct FastArgs {
     int32_t rotary_lanes;          // (HALF) lanes of a head that hold pairs
     int32_t lanes;                 // lanes of a head that hold channels
     int32_t nv[2], parts_q;        // vectors of a token's queries and keys; how many waves share the queries
+    int32_t tokens_log[2];         // (TOKENS) tokens to a wave (log2)
+    int32_t pairs_log;             // (TOKENS) room for a token's angles (log2)
     int32_t write_through;         // how the outputs leave (see stores_through)
     float inv_n[2];                // 1 / (channels under a norm)
 };
@@ -216,10 +219,14 @@ template <int CH> __device__ __forceinline__ void group_sum(float (&v)[CH], int 
 
 // SPLIT (the norm of a row of several waves): a workgroup has one token's queries or its keys; its waves share the angles and add up their sums.
 // Against one wave that holds the whole row, us for 80 heads of 128 bf16: one token 7.2 -> 3.4, 1560 18.0 -> 13.4, 4680 53.5 -> 44.7.
+// TOKENS (few heads, many tokens): the wave's one vector has 2^tokens_log tokens side by side, each with its heads.
 constexpr int MOST_WAVES = 16, MOST_VECTORS = 64;
-template <typename T, int CH, bool HALF, int NORM, bool WHOLE, bool SPLIT>
-__global__ __launch_bounds__(SPLIT ? 64 * MOST_WAVES : TPB) void heads_kernel(FastArgs f)
+enum Mode { PLAIN, SPLIT_ROW, SEVERAL_TOKENS };
+template <typename T, int CH, bool HALF, int NORM, bool WHOLE, Mode MODE>
+__global__ __launch_bounds__(MODE == SPLIT_ROW ? 64 * MOST_WAVES : TPB) void heads_kernel(FastArgs f)
 {
+    constexpr bool SPLIT = MODE == SPLIT_ROW, TOKENS = MODE == SEVERAL_TOKENS;
+    static_assert(!TOKENS || CH == 1, "");
     typedef typename Four<T>::raw raw;
     constexpr bool WIDE = WHOLE && !HALF && sizeof(T) == 2;         // the eight channels are one 16-byte piece
     constexpr bool APART = !HALF && sizeof(T) == 4;
@@ -227,12 +234,15 @@ __global__ __launch_bounds__(SPLIT ? 64 * MOST_WAVES : TPB) void heads_kernel(Fa
     __shared__ float red[SPLIT ? MOST_VECTORS : 1];
     const HeadArgs &a = f.h;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int m = SPLIT ? blockIdx.x : blockIdx.x * (TPB / 64) + wave;
-    if (m >= a.M) return;
     const bool keys = (int)blockIdx.y >= f.parts_q;
     const Tensor &t = a.t[keys];
+    const int tokens_log = TOKENS ? f.tokens_log[keys] : 0;
+    if (SPLIT ? false : ((int64_t)(blockIdx.x * (TPB / 64) + wave) << tokens_log) >= a.M) return;
+    const int m = SPLIT ? blockIdx.x : (blockIdx.x * (TPB / 64) + wave) << tokens_log;       // (the wave's first token)
     const int first = (SPLIT ? wave : (int)blockIdx.y - (keys ? f.parts_q : 0)) * CH;     // vector
-    const int j = lane & ((1 << f.lph_log) - 1), sub = lane >> f.lph_log;
+    const int heads_log = f.hpv_log - tokens_log;
+    const int j = lane & ((1 << f.lph_log) - 1), sub = (lane >> f.lph_log) & ((1 << heads_log) - 1);
+    const int token = TOKENS ? lane >> (f.lph_log + heads_log) : 0;
     const bool rotary = 4 * j < a.pairs;
     const int rest = HALF ? 2 * a.pairs + 8 * (j - f.rotary_lanes) : 8 * j;       // first channel of a lane with eight neighbours
     const int c0 = APART || (HALF && rotary) ? 4 * j : rest, apart = APART ? 4 * f.lanes : HALF && rotary ? a.pairs : 4;
@@ -243,10 +253,11 @@ __global__ __launch_bounds__(SPLIT ? 64 * MOST_WAVES : TPB) void heads_kernel(Fa
         n0 = some(min(a.D, apart) - c0);
         n1 = some(a.D - apart - c0);
     }
-    const bool inside = n0 > 0;
+    const bool inside = n0 > 0 && (!TOKENS || (unsigned)(m + token) < (unsigned)a.M);
     auto pair = [&](int k) { return APART ? 2 * j + (k & 1) + (k & 2) * f.lanes : 4 * j + k; };       // of the lane's four
 
     const T *x = reinterpret_cast<const T *>(t.x) + (size_t)m * t.ld + c0;
+    if (TOKENS) x += token * t.ld;
     raw v[CH][2];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
@@ -280,7 +291,15 @@ __global__ __launch_bounds__(SPLIT ? 64 * MOST_WAVES : TPB) void heads_kernel(Fa
     if (NORM == QARVD_NORM_HEAD && t.w && inside) load_weights(t.w + c0);
 
     float *const mine = turns[SPLIT ? 0 : wave];
-    if (a.pairs) {
+    if (TOKENS && a.pairs) {
+        for (int i = lane; i < 1 << (tokens_log + f.pairs_log); i += 64) {
+            const int p = i & ((1 << f.pairs_log) - 1), at = (int)min((unsigned)(m + (i >> f.pairs_log)), (unsigned)a.M - 1);
+            if (p >= a.pairs) continue;
+            const float2 cs = cos_sin(a.pos[(size_t)at * a.ldpos + axis_of(a, p)], a.freq[p]);
+            mine[i] = cs.x;
+            mine[MAX_D / 2 + i] = cs.y;
+        }
+    } else if (a.pairs) {
         const int32_t *pos = a.pos + (size_t)m * a.ldpos;
         for (int i = SPLIT ? threadIdx.x : lane; i < a.pairs; i += SPLIT ? blockDim.x : 64) {
             const float2 cs = cos_sin(pos[axis_of(a, i)], a.freq[i]);
@@ -302,7 +321,7 @@ __global__ __launch_bounds__(SPLIT ? 64 * MOST_WAVES : TPB) void heads_kernel(Fa
         }
         if constexpr (NORM == QARVD_NORM_ROW) {
             // a sum for each vector, and those in an order of their numbers: the same bits however many tokens there are and waves share the row
-            group_sum<CH>(scale, 6);
+            group_sum<CH>(scale, 6 - tokens_log);
             float sum[1] = {scale[0]};
             if constexpr (SPLIT) {
 #pragma unroll
@@ -330,8 +349,9 @@ __global__ __launch_bounds__(SPLIT ? 64 * MOST_WAVES : TPB) void heads_kernel(Fa
         if (!SPLIT) __builtin_amdgcn_wave_barrier();       // (one wave's LDS accesses complete in order)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            co[k] = mine[pair(k)];
-            si[k] = mine[MAX_D / 2 + pair(k)];
+            const int p = TOKENS ? (token << f.pairs_log) + (pair(k) & ((1 << f.pairs_log) - 1)) : pair(k);
+            co[k] = mine[p];
+            si[k] = mine[MAX_D / 2 + p];
         }
     }
 
@@ -359,7 +379,7 @@ __global__ __launch_bounds__(SPLIT ? 64 * MOST_WAVES : TPB) void heads_kernel(Fa
                 e[q] = turn ? zp : z;
             }
         }
-        const int64_t at = (int64_t)head * t.hs_out + c0;      // from the token's first element
+        const int64_t at = (TOKENS ? token * t.ld_out : 0) + (int64_t)head * t.hs_out + c0;      // from the (first) token's first element
         const raw lo = Four<T>::pack(e), hi = Four<T>::pack(e + 4);
         if constexpr (!WHOLE) {
             store_some<T>(out + at, n0, lo);
@@ -392,11 +412,17 @@ template <typename T, bool HALF, int NORM, bool WHOLE> void launch_fast(const Fa
         constexpr int CH = decltype(n)::value;
         if constexpr (NORM == QARVD_NORM_ROW)
             if (waves > 1) {
-                hipLaunchKernelGGL((heads_kernel<T, CH, HALF, NORM, WHOLE, true>), dim3(f.h.M, f.nv[1] ? 2 : 1), dim3(64 * waves), 0, st, f);
+                hipLaunchKernelGGL((heads_kernel<T, CH, HALF, NORM, WHOLE, SPLIT_ROW>), dim3(f.h.M, f.nv[1] ? 2 : 1), dim3(64 * waves), 0, st, f);
                 return;
             }
-        const dim3 grid((f.h.M + TPB / 64 - 1) / (TPB / 64), f.parts_q + (f.nv[1] + ch - 1) / ch);
-        hipLaunchKernelGGL((heads_kernel<T, CH, HALF, NORM, WHOLE, false>), grid, dim3(TPB), 0, st, f);
+        const int per = (TPB / 64) << (f.nv[1] ? std::min(f.tokens_log[0], f.tokens_log[1]) : f.tokens_log[0]);
+        const dim3 grid((unsigned)(((int64_t)f.h.M + per - 1) / per), f.parts_q + (f.nv[1] + ch - 1) / ch);
+        if constexpr (CH == 1)
+            if (f.tokens_log[0] + f.tokens_log[1] > 0) {
+                hipLaunchKernelGGL((heads_kernel<T, CH, HALF, NORM, WHOLE, SEVERAL_TOKENS>), grid, dim3(TPB), 0, st, f);
+                return;
+            }
+        hipLaunchKernelGGL((heads_kernel<T, CH, HALF, NORM, WHOLE, PLAIN>), grid, dim3(TPB), 0, st, f);
     };
     switch (ch) {
     case 1: return go(std::integral_constant<int, 1>{});
@@ -410,6 +436,7 @@ template <typename T, bool HALF, int NORM, bool WHOLE> void launch_fast(const Fa
 // and 6: 4680 x 24 heads of 128 bf16 14.3, 13.9, 12.3, 12.3, 12.3; 1560 x 24 5.97, 5.60, 5.60, 5.63, 5.66; 520 x 80 fp32 8.98, 8.77, 8.73, 9.05, 9.47;
 // 64 x 24 2.71, 2.87, 3.10, 3.12, 3.12; one token 2.41, 2.55, 2.82, 2.81, 2.81.
 constexpr int64_t WAVES = 4096;
+constexpr int TOKEN_WAVES = 2048;
 
 // Stores that write through the L2, or such with the non-temporal hint.  Nothing is left to write back when the kernel ends with either; written
 // through, the last-level cache (256 MB) still has the outputs for attention.  us plain, through, non-temporal, and the same with a copy of the
@@ -420,7 +447,8 @@ int32_t stores_through(const HeadArgs &a, size_t esz)
     size_t bytes = 0;
     for (const Tensor &t : a.t) {
         bytes += 2 * (size_t)a.M * t.heads * a.D * esz;
-        if (t.heads > 1 && (t.heads - 1) * t.hs_out * (int64_t)esz > 0x7f000000) return 0;      // (32-bit offsets from the token)
+        // (32-bit offsets from a wave's first token)
+        if (((t.heads > 1 ? (t.heads - 1) * t.hs_out : 0) + (a.M > 1 ? 63 * t.ld_out : 0)) * (int64_t)esz > 0x7f000000) return 0;
     }
     return bytes <= ((size_t)256 << 20) ? 1 : 0;
 }
@@ -448,6 +476,11 @@ template <typename T> qarvd_status launch(const HeadArgs &a, hipStream_t st)
             f.inv_n[i] = 1.0f / (float)(a.norm == QARVD_NORM_ROW ? (int64_t)a.t[i].heads * a.D : (int64_t)a.D);
         }
         const int most = f.nv[0] > f.nv[1] ? f.nv[0] : f.nv[1];
+        for (int i = 0; i < 2; ++i) {
+            f.tokens_log[i] = most == 1 && a.t[i].heads ? f.hpv_log - ceil_log2(a.t[i].heads) : 0;
+            while (f.tokens_log[i] && a.M >> f.tokens_log[i] < TOKEN_WAVES) --f.tokens_log[i];
+        }
+        f.pairs_log = ceil_log2(a.pairs);
         const int64_t vectors = (int64_t)a.M * (f.nv[0] + f.nv[1]);
         const int want = vectors >= 4 * WAVES ? 4 : vectors >= 2 * WAVES ? (int)(vectors / WAVES) : 1;
         const bool row = a.norm == QARVD_NORM_ROW;
