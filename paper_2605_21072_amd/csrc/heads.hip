@@ -226,7 +226,6 @@ template <typename T, int CH, bool HALF, int NORM, bool WHOLE, Mode MODE>
 __global__ __launch_bounds__(MODE == SPLIT_ROW ? 64 * MOST_WAVES : TPB) void heads_kernel(FastArgs f)
 {
     constexpr bool SPLIT = MODE == SPLIT_ROW, TOKENS = MODE == SEVERAL_TOKENS;
-    static_assert(!TOKENS || CH == 1, "");
     typedef typename Four<T>::raw raw;
     constexpr bool WIDE = WHOLE && !HALF && sizeof(T) == 2;         // the eight channels are one 16-byte piece
     constexpr bool APART = !HALF && sizeof(T) == 4;
@@ -417,7 +416,7 @@ template <typename T, bool HALF, int NORM, bool WHOLE> void launch_fast(const Fa
             }
         const int per = (TPB / 64) << (f.nv[1] ? std::min(f.tokens_log[0], f.tokens_log[1]) : f.tokens_log[0]);
         const dim3 grid((unsigned)(((int64_t)f.h.M + per - 1) / per), f.parts_q + (f.nv[1] + ch - 1) / ch);
-        if constexpr (CH == 1)
+        if constexpr (CH == 1 || sizeof(T) == 2)
             if (f.tokens_log[0] + f.tokens_log[1] > 0) {
                 hipLaunchKernelGGL((heads_kernel<T, CH, HALF, NORM, WHOLE, SEVERAL_TOKENS>), grid, dim3(TPB), 0, st, f);
                 return;
@@ -436,7 +435,11 @@ template <typename T, bool HALF, int NORM, bool WHOLE> void launch_fast(const Fa
 // and 6: 4680 x 24 heads of 128 bf16 14.3, 13.9, 12.3, 12.3, 12.3; 1560 x 24 5.97, 5.60, 5.60, 5.63, 5.66; 520 x 80 fp32 8.98, 8.77, 8.73, 9.05, 9.47;
 // 64 x 24 2.71, 2.87, 3.10, 3.12, 3.12; one token 2.41, 2.55, 2.82, 2.81, 2.81.
 constexpr int64_t WAVES = 4096;
-constexpr int TOKEN_WAVES = 2048;
+// Where a tensor's heads leave room in their one vector, as many tokens in it as leave this many waves (a wave works out its tokens' angles one after
+// another).  us for 512, 1024, 2048 waves and one token each: 4680 x (1 + 1) heads of 32 bf16 3.3, 3.3, 4.1, 5.2; 1560 of them 3.0, 3.5, 3.5, 3.5; 4680 x
+// (1 + 1) of 128 4.8, 4.8, 4.6, 5.2; 32760 x (2 + 2) of 64 10.1, 10.2, 10.0, 20.9; with all that fit, 520 x (1 + 1) of 128 3.8 instead of 2.9.  bf16
+// keys of few heads also beside queries of up to four vectors: 32760 x (12 + 1) of 128 49.3 -> 45.3, 4680 8.0 -> 8.1 (fp32 79.9 -> 78.2, 10.8 -> 11.4: not built).
+constexpr int TOKEN_WAVES = 1024;
 
 // Stores that write through the L2, or such with the non-temporal hint.  Nothing is left to write back when the kernel ends with either; written
 // through, the last-level cache (256 MB) still has the outputs for attention.  us plain, through, non-temporal, and the same with a copy of the
@@ -477,7 +480,7 @@ template <typename T> qarvd_status launch(const HeadArgs &a, hipStream_t st)
         }
         const int most = f.nv[0] > f.nv[1] ? f.nv[0] : f.nv[1];
         for (int i = 0; i < 2; ++i) {
-            f.tokens_log[i] = most == 1 && a.t[i].heads ? f.hpv_log - ceil_log2(a.t[i].heads) : 0;
+            f.tokens_log[i] = f.nv[i] == 1 && (most == 1 || (sizeof(T) == 2 && most <= 4)) ? f.hpv_log - ceil_log2(a.t[i].heads) : 0;
             while (f.tokens_log[i] && a.M >> f.tokens_log[i] < TOKEN_WAVES) --f.tokens_log[i];
         }
         f.pairs_log = ceil_log2(a.pairs);

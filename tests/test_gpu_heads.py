@@ -64,7 +64,7 @@ SHAPES = [(1, 12, 12, 128, (44, 42, 42)), (37, 12, 12, 128, (44, 42, 42)), (5, 4
           (2, 72, 72, 128, (44, 42, 42)), (6, 33, 5, 104, (52, 52)), (2, 260, 3, 128, (44, 42, 42)), (3, 2, 2, 511, (20,)), (5, 50, 50, 256, (64, 96, 96)),
           (3, 64, 64, 512, (512,)), (500, 40, 8, 128, (44, 42, 42)), (1100, 40, 20, 100, (20, 22, 18)),
           (4100, 1, 2, 64, (32, 32)), (9001, 3, 1, 40, (40,)), (70001, 1, 1, 8, (4, 2, 2)), (8193, 2, 2, 33, (16, 16)), (20000, 1, 4, 100, (20, 22, 18)), (4500, 2, 1, 128, (128,)),
-          (66000, 5, 1, 1, ())]
+          (66000, 5, 1, 1, ()), (4500, 12, 1, 128, (44, 42, 42)), (2100, 10, 3, 100, (20, 22, 18)), (5000, 1, 17, 64, (64,))]
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
