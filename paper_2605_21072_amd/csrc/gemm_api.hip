@@ -334,8 +334,8 @@ extern "C" qarvd_status qarvd_w8a8_dual_gemm_q8(const int8_t *Xq, int64_t ldxq, 
 namespace {
 struct FusedVariant {
     int BM, BN, bits;
-    int form;           // 0: as the aligned tiles need it, 1: strides up to 2^22, 2: anything, 3: at most BM rows
-    double c, a, b;     // cost model of pick_variant
+    int form;           // 0: as the aligned tiles need it, 1: strides up to 2^22, 2: anything, 3: anything, for few tokens (see pick_rows)
+    double c, a, b;     // cost model of pick_variant; form 3: c is the workgroups to a CU up to which it is taken
     double gelu, res;   // what GELU, or a gate and a residual, add to a tile's epilogue (a)
     qarvd_status (*launch)(const GemmArgs &, qarvd_dtype, hipStream_t);
 };
@@ -357,15 +357,12 @@ const FusedVariant kFusedVariants[] = {
     {128, 128, 4, 1, 2.74, 3.47, 0.196, 0.6, 2.4, launch_dma128_fused<128, 128, 2, 4, 3, true, true>},
     {64, 64, 4, 1, 3.60, 1.00, 0.101, 0.1, 1.0, launch_dma128_fused<64, 64, 2, 2, 3, true, true>},
     {128, 128, 4, 2, 0, 0, 0, 0, 0, launch_staged_fused<true>},
-    {8, 8, 8, 3, 0, 0, 0, 0, 0, launch_rows_gemm<1, 1, 2, false>},
-    {16, 16, 8, 3, 0, 0, 0, 0, 0, launch_rows_gemm<1, 1, 1, false>},
-    {16, 32, 8, 3, 0, 0, 0, 0, 0, launch_rows_gemm<1, 2, 1, false>},
-    {32, 16, 8, 3, 0, 0, 0, 0, 0, launch_rows_gemm<2, 1, 1, false>},
-    {8, 8, 4, 3, 0, 0, 0, 0, 0, launch_rows_gemm<1, 1, 2, true>},
-    {16, 16, 4, 3, 0, 0, 0, 0, 0, launch_rows_gemm<1, 1, 1, true>},
-    {16, 32, 4, 3, 0, 0, 0, 0, 0, launch_rows_gemm<1, 2, 1, true>},
-    {32, 16, 4, 3, 0, 0, 0, 0, 0, launch_rows_gemm<2, 1, 1, true>},
-    {32, 32, 4, 3, 0, 0, 0, 0, 0, launch_rows_gemm<2, 2, 1, true>},
+    {8, 8, 8, 3, 1, 0, 0, 0, 0, launch_rows_gemm<1, 1, 2, false>},
+    {16, 16, 8, 3, 1, 0, 0, 0, 0, launch_rows_gemm<1, 1, 1, false>},
+    {32, 16, 8, 3, 1, 0, 0, 0, 0, launch_rows_gemm<2, 1, 1, false>},
+    {8, 8, 4, 3, 1, 0, 0, 0, 0, launch_rows_gemm<1, 1, 2, true>},
+    {16, 16, 4, 3, 1, 0, 0, 0, 0, launch_rows_gemm<1, 1, 1, true>},
+    {16, 32, 4, 3, 2, 0, 0, 0, 0, launch_rows_gemm<1, 2, 1, true>},
 };
 constexpr int kNumFusedVariants = sizeof(kFusedVariants) / sizeof(kFusedVariants[0]);
 
@@ -396,17 +393,22 @@ qarvd_status fill_ending(const qarvd_ending *e, qarvd_dtype ydt, GemmArgs *g)
     return QARVD_OK;
 }
 
-// Kernels for few rows (gemm_rows.hip): the narrowest whose workgroups all have a CU, up to sixteen rows also more of them than CUs where the weights
-// are INT4.  Wider outputs are the tiles': us at their limits, rows and best tile, INT8 1 x 1536 -> 8960 7.3 and 6.8, 16 x 1536 -> 8960 10.6 and
-// 6.8, 32 x 1536 -> 4608 8.3 and 7.0; INT4 16 x 4096 -> 13824 12.2 and 15.4, 32 x 4096 -> 4608 11.1 and 12.8, 32 x 4096 -> 8960 14 and 13.  0: none.
+// Kernels for few tokens (gemm_rows.hip): the first whose workgroups all run side by side; up to sixteen tokens also with more of them, where the weights
+// are most of the bytes.  Over 33 to 384 tokens of K 1024 to 8960 and N 64 to 5120 the rule is within 0.4 % (INT4 1.4 %) of the best kernel on
+// average, over 2 to 32 tokens within 0.3 % (1.5 %); without these kernels the calls take 1.21 (1.54) and 1.47 (2.1) times as long.  us, rows and best tile, on either
+// side of the limits: INT8 8 x 8, 256 x 8960 -> 64 7.7 and 16.7, 384 x 8960 -> 64 11.7 (16 x 16 11.4); 16 x 16, 96 x 4096 -> 640 7.5 and 10.8, 128 x 4096
+// -> 640 11.1 and 10.9; 32 x 16, 192 x 4096 -> 640 9.7 and 10.9, 256 x 4096 -> 640 16.8 and 11.0; 16 x 1024 -> 8000 6.2 and 7; INT4 16 x 32, 96 x 4096 -> 2560
+// 11.2 and 14.0, 16 x 4096 -> 13824 12.2 and 15.4.  0: none.
 int32_t pick_rows(int bits, const GemmArgs &g)
 {
     const int cus = device_cus();
     for (int i = 0; i < kNumFusedVariants; ++i) {
         const FusedVariant &v = kFusedVariants[i];
-        if (v.form != 3 || v.bits != bits || g.M > v.BM || (v.BM == 32 && g.M <= 16)) continue;
-        const bool widest = v.BM == 16 && v.BN == 32;
-        if (g.N <= v.BN * cus || (widest && bits == 4)) return i + 1;
+        if (v.form != 3 || v.bits != bits || (v.BM == 32 && g.M <= 16)) continue;
+        const int64_t workgroups = (int64_t)((g.N + v.BN - 1) / v.BN) * ((g.M + v.BM - 1) / v.BM);
+        double most = v.c * cus;
+        if (g.M <= 16 && v.BM == 16) most = bits == 8 ? 2.0 * cus : v.BN == 32 ? 1e9 : most;
+        if ((double)workgroups <= most) return i + 1;
     }
     return 0;
 }
@@ -442,7 +444,7 @@ qarvd_status launch_fused(int bits, int32_t variant, const GemmArgs &g, qarvd_dt
         variant = cheapest(cand, n, g);
     }
     const FusedVariant &v = kFusedVariants[variant - 1];
-    if (v.bits != bits || (v.form == 0 && !(g.n_off <= 128 && g.vec_out)) || (v.form == 1 && !short_rows_ok(g)) || (v.form == 3 && g.M > v.BM) ||
+    if (v.bits != bits || (v.form == 0 && !(g.n_off <= 128 && g.vec_out)) || (v.form == 1 && !short_rows_ok(g)) || (v.form == 3 && g.M > 65535LL * v.BM) ||
         !gates_fit(v, g))
         return QARVD_ERR_UNSUPPORTED;
     return v.launch(g, ydt, reinterpret_cast<hipStream_t>(stream));

@@ -1,5 +1,5 @@
-// Few tokens: the dual-scale GEMM with its fused ending for up to 32 rows, where the weights are all the bytes and the tiles of gemm_dma128.h
-// leave most CUs without work (1536 outputs are 24 of its smallest) and walk the whole of K one stage after another.
+// Few tokens, or few outputs: the dual-scale GEMM with its fused ending where the tiles of gemm_dma128.h leave most CUs without work (one token's 1536
+// outputs are 24 of its smallest) and walk the whole of K one stage after another.
 //
 // A workgroup has CT times 16 output columns and MT times 16 rows; its eight waves share K: spans of 128 packed positions (one cache line of an INT8
 // row), wave w every eighth.  Operands go from memory to the matrix instructions without LDS: in v_mfma_i32_16x16x64_i8 lane l supplies sixteen K
@@ -7,15 +7,18 @@
 // of a span, two instructions' worth, 32 bytes of INT8 or 16 of INT4 in one piece.  Four spans of a wave are in flight; what a span has
 // delivered is multiplied and its registers are asked to hold the fourth next.  The outlier range ends at a multiple of 32: a quarter lies on one side of it.
 //
-// P = 2, for up to eight rows: the sixteen rows of either operand are eight of one span and the same eight of the next.  Of the 16 x 16 products
+// P = 2, eight rows: the sixteen rows of either operand are eight of one span and the same eight of the next.  Of the 16 x 16 products
 // the two 8 x 8 blocks whose spans agree are sums of the result; the others are left.  A workgroup then has eight columns, there are twice as many,
 // and still every lane fetches weights of its own.
 //
 // Sums are integers, so the waves add theirs in LDS in any order, and the epilogue is the tiles' own arithmetic: the same bits.
 //
+// Operands are read again by every workgroup that shares them, at 16 multiplications to a byte at most: once the workgroups no longer all run side by
+// side, tiles that pass operands through LDS are faster (the choice and what it measured: pick_rows).
+//
 // Bound by the latency of the first loads (2 us of launch and epilogue, about 2 us until the weights are there) and beyond a few MB by how much 256 CUs
-// keep in flight.  us against the best tile, INT8 weights: 1 x 1536 -> 1536 3.7 (6.4), 1 x 8960 -> 1536 5.8 (16), 16 x 8960 -> 1536 11.7 (16.4),
-// 1 x 13824 -> 4608 17 (28.7); INT4: 1 x 8960 -> 1536 4.6 (21), 16 x 4096 -> 8960 10.7 (13), 32 x 8960 -> 1536 12.9 (21).
+// keep in flight.  us against the best tile, INT8 weights: 1 x 1536 -> 1536 3.7 (6.4), 1 x 8960 -> 1536 5.8 (16), 16 x 8960 -> 1536 12.1 (16.9),
+// 1 x 13824 -> 4608 17 (28.7); INT4: 1 x 8960 -> 1536 4.6 (21), 16 x 4096 -> 8960 10.7 (13), 32 x 8960 -> 1536 9.5 (22.6).
 #include <type_traits>
 
 #include "gemm_dma_common.h"
@@ -145,7 +148,7 @@ __global__ __launch_bounds__(64 * NW) void gemm_rows_kernel(GemmArgs g, RowsX in
     extern __shared__ __align__(16) unsigned char image[];      // (QUANT) the packed row, then the row in natural order
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & (PER - 1), part = (lane & 15) / PER, q = lane >> 4;
-    const int n0 = blockIdx.x * COLS;
+    const int n0 = blockIdx.x * COLS, m0 = blockIdx.y * ROWS, rows = min(ROWS, g.M - m0);
     const int spans = g.kp / SPAN;
     const int8_t *pw[CT], *px[MT];
 #pragma unroll
@@ -154,7 +157,7 @@ __global__ __launch_bounds__(64 * NW) void gemm_rows_kernel(GemmArgs g, RowsX in
 #pragma unroll
     for (int t = 0; t < MT; ++t)
         px[t] = QUANT ? reinterpret_cast<const int8_t *>(image) + q * 32
-                      : g.Xq + (size_t)min(t * 16 + r, g.M - 1) * g.ldxq + q * 32;
+                      : g.Xq + (size_t)(m0 + min(t * 16 + r, rows - 1)) * g.ldxq + q * 32;
 
     v4i acc[2][MT][CT];
 #pragma unroll
@@ -167,7 +170,7 @@ __global__ __launch_bounds__(64 * NW) void gemm_rows_kernel(GemmArgs g, RowsX in
     auto load_x = [&](int u, int s) {                // s: this lane's span
 #pragma unroll
         for (int t = 0; t < MT; ++t)
-            if (s < spans && t * 16 + r < g.M) {     // lanes of rows that do not exist fetch nothing
+            if (s < spans && t * 16 + r < rows) {     // lanes of rows that do not exist fetch nothing
                 const v4i *b = reinterpret_cast<const v4i *>(px[t] + (size_t)s * SPAN);
                 x[u][t][0] = b[0];
                 x[u][t][1] = b[1];
@@ -236,7 +239,7 @@ __global__ __launch_bounds__(64 * NW) void gemm_rows_kernel(GemmArgs g, RowsX in
             for (int e = 0; e < 4; ++e) {
                 // this lane: token row r of its part, column 4 q + e, which is of another part where the two K ranges differ
                 const int col = (4 * q + e) & (PER - 1);
-                if (t * 16 + r >= g.M || (4 * q + e) / PER != part) continue;
+                if (t * 16 + r >= rows || (4 * q + e) / PER != part) continue;
                 if (wave * P * SPAN < g.n_off) atomicAdd(&sums[0][t * PER + r][PER * c + col], acc[0][t][c][e]);      // (the waves that saw outliers)
                 atomicAdd(&sums[1][t * PER + r][PER * c + col], acc[1][t][c][e]);
             }
@@ -245,11 +248,11 @@ __global__ __launch_bounds__(64 * NW) void gemm_rows_kernel(GemmArgs g, RowsX in
     OutT *const Y = reinterpret_cast<OutT *>(g.Y);
     const OutT *const R = reinterpret_cast<const OutT *>(g.R);
     for (int i = tid; i < ROWS * COLS; i += 64 * NW) {
-        const int m = i / COLS, c = i % COLS, n = n0 + c;
-        if (m >= g.M || n >= g.N) continue;
+        const int row = i / COLS, m = m0 + row, c = i % COLS, n = n0 + c;
+        if (row >= rows || n >= g.N) continue;
         constexpr float ws = W4 ? 0.0625f : 1.0f;     // INT4 codes enter the matrix instructions times 16
-        float v = (float)sums[0][m][c] * (g.n_off > 0 ? g.s_o[n] * ws : 0.0f);
-        v = fmaf((float)sums[1][m][c], g.s_n[n] * ws, v);
+        float v = (float)sums[0][row][c] * (g.n_off > 0 ? g.s_o[n] * ws : 0.0f);
+        v = fmaf((float)sums[1][row][c], g.s_n[n] * ws, v);
         v = fmaf(v, QUANT ? own_scale : g.s_x[m], g.bias ? g.bias[n] : 0.0f);
         if (g.act == QARVD_ACT_GELU_TANH) v = gelu_tanh(v);
         if (g.gate || g.R) {
@@ -269,8 +272,8 @@ __global__ __launch_bounds__(64 * NW) void gemm_rows_kernel(GemmArgs g, RowsX in
 
 template <int MT, int CT, int P, bool W4> qarvd_status launch_rows_gemm(const GemmArgs &g, qarvd_dtype ydt, hipStream_t st)
 {
-    constexpr int COLS = 16 / P * CT;
-    const dim3 grid((g.N + COLS - 1) / COLS), block(64 * NW);
+    constexpr int COLS = 16 / P * CT, ROWS = 16 / P * MT;
+    const dim3 grid((g.N + COLS - 1) / COLS, (g.M + ROWS - 1) / ROWS), block(64 * NW);
     if (ydt == QARVD_BF16) hipLaunchKernelGGL((gemm_rows_kernel<MT, CT, P, W4, uint16_t, void>), grid, block, 0, st, g, RowsX{});
     else hipLaunchKernelGGL((gemm_rows_kernel<MT, CT, P, W4, float, void>), grid, block, 0, st, g, RowsX{});
     return qarvd_launch_status();
@@ -301,12 +304,9 @@ template qarvd_status launch_rows_quant<true>(const GemmArgs &, const void *, qa
 #define QARVD_INST_ROWS(MT, CT, P, W4) template qarvd_status launch_rows_gemm<MT, CT, P, W4>(const GemmArgs &, qarvd_dtype, hipStream_t);
 QARVD_INST_ROWS(1, 1, 2, false)
 QARVD_INST_ROWS(1, 1, 1, false)
-QARVD_INST_ROWS(1, 2, 1, false)
 QARVD_INST_ROWS(2, 1, 1, false)
 QARVD_INST_ROWS(1, 1, 2, true)
 QARVD_INST_ROWS(1, 1, 1, true)
 QARVD_INST_ROWS(1, 2, 1, true)
-QARVD_INST_ROWS(2, 1, 1, true)
-QARVD_INST_ROWS(2, 2, 1, true)
 
 }  // namespace qarvd_gemm
