@@ -299,7 +299,7 @@ int32_t qarvd_q8_gemm_num_variants(void);
  *     a      = y, or gelu_tanh(y) as defined above
  *     Y[m,n] = fmaf(gate[m / gate_rows, n], a, residual[m,n])     stored as fp32, or rounded to bf16 once
  * A missing residual is +0, a missing gate 1; with neither, Y is `a` itself.  GELU is evaluated in fp32 with one hardware 2^t and
- * one hardware reciprocal per value; it lies within 4e-7 + 2e-6 |gelu(y)| of the real-valued function.
+ * one hardware reciprocal per value; it lies within 4e-7 + 2e-6 |gelu(y)| of the real-valued function.  Every kernel gives the same bits.
  *   act        QARVD_ACT_NONE or QARVD_ACT_GELU_TANH
  *   gate       in  f32 [groups, ldg] or NULL: tokens m with the same m / gate_rows share a row (one modulation vector per frame:
  *              gate_rows = its tokens); the last group may be shorter.  gate_rows >= 1; gate_rows >= M: one row, ldg is ignored
