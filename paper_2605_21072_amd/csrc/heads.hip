@@ -42,19 +42,29 @@ template <> __device__ __forceinline__ uint16_t narrow1<uint16_t>(float v)      
     return (uint16_t)__builtin_bit_cast(uint32_t, __builtin_convertvector(f, v2bf));
 }
 
-// Cosine and sine of pos * freq.  The product and its reduction to [-1/2, 1/2] turns are fp64: a position of 2^31 leaves an angle that is off by
-// 4e-7.  What remains is split into a whole number of quarter turns and a rest of at most an eighth, which fp32 holds to 2e-8.
+// Cosine and sine of pos * freq.  The angle in quarter turns and its reduction to [-1/2, 1/2] are fp64: a position of 2^31 leaves an angle that is off by
+// 5e-7.  1.5 2^52 added puts the nearest whole number into the low bits.  The rest, at most an eighth of a turn, is fp32 (off by 5e-8); its sine and
+// cosine are their Taylor series to z^9 and z^10, whose next terms are below 2e-9 there.  Where a wave has little else to do it is most of the instructions: with
+// the library's function of any argument and a reduction to a turn before that to a quarter, us: 32760 x (1 + 1) heads of 128 14.6 instead of 11.7,
+// 1560 x (12 + 12) rotated alone 4.6 instead of 4.1.
 __device__ __forceinline__ float2 cos_sin(int pos, double freq)
 {
-    double t = (double)pos * freq * 0.15915494309189535;
-    t -= rint(t);
-    const double quarters = rint(4.0 * t);
-    const float rest = (float)(4.0 * t - quarters);
-    float s, c;
-    sincospif(0.5f * rest, &s, &c);
-    const int k = (int)quarters & 3;
+    constexpr double MAGIC = 6755399441055744.0;
+    const double quarters = (double)pos * freq * 0.63661977236758134;
+    const double rounded = quarters + MAGIC;
+    const float z = (float)(quarters - (rounded - MAGIC)) * 1.57079632679f, z2 = z * z;
+    const unsigned k = (unsigned)__double_as_longlong(rounded);
+    float s = fmaf(z2, 2.7557319e-6f, -1.9841270e-4f);
+    s = fmaf(z2, s, 8.3333333e-3f);
+    s = fmaf(z2, s, -0.16666667f);
+    s = fmaf(z * z2, s, z);
+    float c = fmaf(z2, -2.7557319e-7f, 2.4801587e-5f);
+    c = fmaf(z2, c, -1.3888889e-3f);
+    c = fmaf(z2, c, 4.1666667e-2f);
+    c = fmaf(z2, c, -0.5f);
+    c = fmaf(z2, c, 1.0f);
     const float x = k & 1 ? s : c, y = k & 1 ? c : s;
-    return make_float2(k == 1 || k == 2 ? -x : x, k >= 2 ? -y : y);
+    return make_float2(__uint_as_float(__float_as_uint(x) ^ (((k + 1) << 30) & 0x80000000u)), __uint_as_float(__float_as_uint(y) ^ ((k << 30) & 0x80000000u)));
 }
 __device__ __forceinline__ int axis_of(const HeadArgs &a, int pair) { return pair < a.end0 ? 0 : pair < a.end1 ? 1 : 2; }
 
