@@ -518,6 +518,10 @@ template <typename T> qarvd_status launch(const HeadArgs &a, hipStream_t st)
     return qarvd_launch_status();
 }
 
+// Tokens of one launch.  It has fewer than 2^32 work-items along x (of a count beyond, only the rest modulo 2^32 would run), and a token has at most
+// 1024 of them.
+constexpr int64_t MOST_TOKENS = 1 << 21;
+
 // One tensor's pointers and strides.  The strides of a single token or a single head say nothing; otherwise the elements must not overlap:
 // a token's heads lie between it and the next, or a head's tokens between it and the next head.
 qarvd_status check_tensor(const qarvd_heads *h, size_t esz, int32_t M, int32_t D)
@@ -571,7 +575,7 @@ extern "C" qarvd_status qarvd_qk_norm_rope(const qarvd_heads *q, const qarvd_hea
         const qarvd_heads *h = i ? k : q;
         a.t[i] = Tensor{h->x, h->out, h->weight, h->ld, h->head_stride, h->ld_out, h->head_stride_out, h->heads};
     }
-    a.eps = eps; a.M = M; a.D = D; a.norm = (int32_t)norm;
+    a.eps = eps; a.D = D; a.norm = (int32_t)norm;
     if (rope) {
         a.pos = rope->pos; a.ldpos = rope->ldpos; a.freq = rope->freq; a.interleaved = rope->interleaved;
         a.end0 = rope->axis_dims[0] / 2;
@@ -579,5 +583,17 @@ extern "C" qarvd_status qarvd_qk_norm_rope(const qarvd_heads *q, const qarvd_hea
         a.pairs = a.end1 + (rope->n_axes > 2 ? rope->axis_dims[2] / 2 : 0);
     }
     hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-    return dt == QARVD_F32 ? launch<float>(a, st) : launch<uint16_t>(a, st);
+    const int64_t esz = dt == QARVD_F32 ? 4 : 2;
+    for (int64_t left = M;;) {
+        a.M = (int32_t)std::min(left, MOST_TOKENS);
+        if (qarvd_status s = dt == QARVD_F32 ? launch<float>(a, st) : launch<uint16_t>(a, st); s != QARVD_OK) return s;
+        left -= a.M;
+        if (left == 0) return QARVD_OK;
+        for (Tensor &t : a.t) {
+            if (!t.heads) continue;
+            t.x = reinterpret_cast<const char *>(t.x) + MOST_TOKENS * t.ld * esz;
+            t.out = reinterpret_cast<char *>(t.out) + MOST_TOKENS * t.ld_out * esz;
+        }
+        if (a.pos) a.pos += MOST_TOKENS * a.ldpos;
+    }
 }
