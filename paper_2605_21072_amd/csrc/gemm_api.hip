@@ -393,6 +393,13 @@ qarvd_status fill_ending(const qarvd_ending *e, qarvd_dtype ydt, GemmArgs *g)
     return QARVD_OK;
 }
 
+// A launch has fewer than 2^32 work-items along x (of a count beyond, only the rest modulo 2^32 would run) and 65535 workgroups along y; the kernels for few
+// tokens have a workgroup of eight waves for each block of the output.  The tiles' grids are bounded by the CUs.
+bool grid_fits(const FusedVariant &v, const GemmArgs &g)
+{
+    return v.form != 3 || ((g.N - 1) / v.BN + 1 < (1 << 23) && g.M <= 65535LL * v.BM);
+}
+
 // Kernels for few tokens (gemm_rows.hip): the first whose workgroups all run side by side; up to sixteen tokens also with more of them, where the weights
 // are most of the bytes.  Over 33 to 384 tokens of K 1024 to 8960 and N 64 to 5120 the rule is within 0.4 % (INT4 1.4 %) of the best kernel on
 // average, over 2 to 32 tokens within 0.3 % (1.5 %); without these kernels the calls take 1.21 (1.54) and 1.47 (2.1) times as long.  us, rows and best tile, on either
@@ -408,7 +415,7 @@ int32_t pick_rows(int bits, const GemmArgs &g)
         const int64_t workgroups = (int64_t)((g.N + v.BN - 1) / v.BN) * ((g.M + v.BM - 1) / v.BM);
         double most = v.c * cus;
         if (g.M <= 16 && v.BM == 16) most = bits == 8 ? 2.0 * cus : v.BN == 32 ? 1e9 : most;
-        if ((double)workgroups <= most) return i + 1;
+        if ((double)workgroups <= most && grid_fits(v, g)) return i + 1;
     }
     return 0;
 }
@@ -444,8 +451,7 @@ qarvd_status launch_fused(int bits, int32_t variant, const GemmArgs &g, qarvd_dt
         variant = cheapest(cand, n, g);
     }
     const FusedVariant &v = kFusedVariants[variant - 1];
-    if (v.bits != bits || (v.form == 0 && !(g.n_off <= 128 && g.vec_out)) || (v.form == 1 && !short_rows_ok(g)) || (v.form == 3 && g.M > 65535LL * v.BM) ||
-        !gates_fit(v, g))
+    if (v.bits != bits || (v.form == 0 && !(g.n_off <= 128 && g.vec_out)) || (v.form == 1 && !short_rows_ok(g)) || !grid_fits(v, g) || !gates_fit(v, g))
         return QARVD_ERR_UNSUPPORTED;
     return v.launch(g, ydt, reinterpret_cast<hipStream_t>(stream));
 }
