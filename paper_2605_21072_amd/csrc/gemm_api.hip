@@ -438,15 +438,19 @@ qarvd_status launch_fused(int bits, int32_t variant, const GemmArgs &g, qarvd_dt
     }
     if (variant == 0) {
         const bool fast_ok = g.n_off <= 128 && g.vec_out;
-        // (INT4: the any-width tiles stand beside the aligned ones, as for the plain GEMM)
         const int form = !short_rows_ok(g) ? 2 : fast_ok && (g.last_group <= 1 || g.gate_rows >= 63) ? 0 : 1;      // (64 rows: the lowest tile)
+        // The any-width tiles stand beside the aligned ones on INT4 weights, as for the plain GEMM, and where groups of tokens are too short for the
+        // aligned tiles of 128 rows: the 64-row tiles alone are the slower ones of a large product and not priced there (cheapest).  us, the best of them
+        // and the any-width 128 x 128, groups of 100 tokens, bf16 residual: 4680 x 5120 -> 5120 187 and 148, 4680 x 13824 -> 5120 419 and 316, 4680 x 8960
+        // -> 1536 96 and 69, 4680 x 1536 -> 1536 25.3 and 23.1.
+        const bool beside = bits == 4 || (g.last_group > 1 && g.gate_rows < 127);
         Cand cand[kNumFusedVariants];
         int n = 0;
         const bool gelu_alone = !g.gate && !g.R;
         for (int i = 0; i < kNumFusedVariants; ++i) {
             const FusedVariant &v = kFusedVariants[i];
             if ((v.BM * v.BN > 128 * 256 && !gelu_alone) || !gates_fit(v, g)) continue;
-            if (v.bits == bits && (v.form == form || (bits == 4 && form == 0 && v.form == 1))) cand[n++] = {i + 1, v.BM, v.BN, v.c, v.a + (g.act == QARVD_ACT_GELU_TANH ? v.gelu : 0.0) + (gelu_alone ? 0.0 : v.res), v.b};
+            if (v.bits == bits && (v.form == form || (beside && form == 0 && v.form == 1))) cand[n++] = {i + 1, v.BM, v.BN, v.c, v.a + (g.act == QARVD_ACT_GELU_TANH ? v.gelu : 0.0) + (gelu_alone ? 0.0 : v.res), v.b};
         }
         variant = cheapest(cand, n, g);
     }

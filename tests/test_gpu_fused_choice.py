@@ -1,0 +1,48 @@
+"""What the heuristic chooses for a fused call, by its time against the kernels by number."""
+import pytest
+import torch
+
+import paper_2605_21072_amd as q
+from test_gpu_fused import layer
+
+pytestmark = pytest.mark.gpu
+
+
+def times(calls, rounds=9, n=6):
+    """Median us of each call, all in turn."""
+    for call in calls:
+        call()
+    got = [[] for _ in calls]
+    for _ in range(rounds):
+        for t, call in zip(got, calls):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            for _ in range(n):
+                call()
+            b.record()
+            b.synchronize()
+            t.append(a.elapsed_time(b) / n * 1e3)
+    return [sorted(t)[rounds // 2] for t in got]
+
+
+@pytest.mark.parametrize("rows", [63, 100, 126])
+@pytest.mark.parametrize("M,K,N", [(4680, 5120, 5120), (4680, 8960, 1536)])
+def test_groups_too_short_for_the_tall_tiles(M, K, N, rows):
+    """More than two groups of 63 to 126 tokens: the choice is not far from the best kernel.  (The best was 1.25 to 1.4 times as fast as the choice where only
+    the aligned tiles of 64 rows were candidates; two timings of one kernel differ by a few percent.)"""
+    w, _ = layer(1, N, K, 64, 8)
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    X, bias = torch.randn((M, K), generator=gen, device="cuda"), torch.randn(N, generator=gen, device="cuda")
+    gate, R = torch.randn((-(-M // rows), N), generator=gen, device="cuda"), torch.randn((M, N), generator=gen, device="cuda").bfloat16()
+    Xq, s_x = q.quant_act(X, w.perm, 64)
+    Y = torch.empty_like(R)
+    call = lambda v: q.w8a8_dual_gemm_fused(Xq, s_x, w, bias, M, gate=gate, gate_rows=rows, residual=R, Y=Y, variant=v)      # noqa: E731
+    able = []
+    for v in range(1, 10):                                  # the tiles of INT8 weights
+        try:
+            call(v)
+            able.append(v)
+        except q.QarvdError:
+            pass
+    chosen, *each = times([lambda v=v: call(v) for v in [0] + able])
+    assert chosen <= 1.15 * min(each), (chosen, dict(zip(able, each)))
