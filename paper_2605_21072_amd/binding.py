@@ -503,6 +503,24 @@ def _vector(t: Optional[torch.Tensor], n: int, what: str):
         raise ValueError("%s must be a contiguous vector of %d" % (what, n))
 
 
+def _array(t: Optional[torch.Tensor], n: int, dtype, what: str):
+    """At least n elements of the type, one behind the other."""
+    if t is not None and t.dtype != dtype:
+        raise TypeError("%s must be %s" % (what, str(dtype)[6:]))
+    if t is not None and (not t.is_contiguous() or t.numel() < n):
+        raise ValueError("%s must be contiguous and hold %d" % (what, n))
+
+
+def _layer(w: DualScaleWeight):
+    """The layer's buffers hold what its sizes say (perm is read only where there are outliers)."""
+    if w.Wq.dim() != 2 or w.Wq.shape[0] < w.N or (w.Wq.shape[1] > 1 and w.Wq.stride(1) != 1):
+        raise ValueError("the layer's Wq must have %d rows with unit inner stride" % w.N)
+    _array(w.s_normal, w.N, torch.float32, "s_normal")
+    _array(w.s_outlier, w.N, torch.float32, "s_outlier")
+    if w.K_o > 0:
+        _array(w.perm, w.K, torch.int32, "perm")
+
+
 def _ending(M: int, N: int, act: int, gate, gate_rows, residual, dtype) -> Optional[_Ending]:
     """Checks of the ending's tensors against the output's shape and type, and the C struct."""
     e = _Ending(int(act), M, None, N, None, N)
@@ -555,13 +573,15 @@ def w8a8_dual_gemm_fused(Xq: torch.Tensor, s_x: torch.Tensor, w: DualScaleWeight
         _check(st, "qarvd_dual_gemm_fused")
         return Y
     dtype = out_dtype if Y is None else Y.dtype
+    _layer(w)
     _vector(bias, w.N, "bias")
     e = _ending(M, w.N, act, gate, gate_rows, residual, dtype)
     if dtype not in _DTYPES:
         raise TypeError("expected float32 or bfloat16, got %s" % dtype)
-    _on_call_device(stream, Xq, s_x, w.Wq, bias, gate, residual, Y)
-    if Xq.dim() != 2 or Xq.shape[0] < M:
-        raise ValueError("Xq has fewer than M rows")
+    _on_call_device(stream, Xq, s_x, w.Wq, w.s_normal, w.s_outlier, bias, gate, residual, Y)
+    if Xq.dim() != 2 or Xq.shape[0] < M or (Xq.shape[1] > 1 and Xq.stride(1) != 1):
+        raise ValueError("Xq must have M rows with unit inner stride")
+    _array(s_x, M, torch.float32, "s_x")
     Y = _out(Y, M, w.N, dtype, Xq.device, stream)
     st = lib.qarvd_dual_gemm_fused(_ptr(Xq), Xq.stride(0), _ptr(s_x), w.bits, _ptr(w.Wq), w.Wq.stride(0), _ptr(w.s_normal), _ptr(w.s_outlier),
                                    _ptr(bias), C.byref(e), M, w.N, w.K, w.K_o, _ptr(Y), _dt(Y), _ld(Y), variant, _stream(stream))
@@ -584,11 +604,12 @@ def w8a8_linear_fused(X: torch.Tensor, w: DualScaleWeight, bias: Optional[torch.
     if K != w.K:
         raise ValueError("X has %d channels, the layer %d" % (K, w.K))
     dtype = out_dtype if Y is None else Y.dtype
+    _layer(w)
     _vector(bias, w.N, "bias")
     e = _ending(M, w.N, act, gate, gate_rows, residual, dtype)
     if dtype not in _DTYPES:
         raise TypeError("expected float32 or bfloat16, got %s" % dtype)
-    _on_call_device(stream, X, w.Wq, bias, gate, residual, Y)
+    _on_call_device(stream, X, w.Wq, w.s_normal, w.s_outlier, w.perm if w.K_o > 0 else None, bias, gate, residual, Y)
     need = lib.qarvd_linear_workspace(M, K, w.K_o)
     ws = _empty(need, torch.uint8, X.device, stream, scratch=True)
     Y = _out(Y, M, w.N, dtype, X.device, stream)
@@ -710,11 +731,12 @@ def w8a8_linear_qkv(X: torch.Tensor, w: DualScaleWeight, bias: Optional[torch.Te
     M, K = X.shape
     if K != w.K:
         raise ValueError("X has %d channels, the layer %d" % (K, w.K))
+    _layer(w)
     _vector(bias, w.N, "bias")
     _norm_weight(weight_q, norm, heads_q, head_dim, "weight_q")
     _norm_weight(weight_k, norm, heads_k, head_dim, "weight_k")
     r = _rope(rope, pos, M)
-    _on_call_device(stream, X, w.Wq, bias, weight_q, weight_k, pos, rope and rope.freq)
+    _on_call_device(stream, X, w.Wq, w.s_normal, w.s_outlier, w.perm if w.K_o > 0 else None, bias, weight_q, weight_k, pos, rope and rope.freq)
     need = lib.qarvd_linear_workspace(M, K, w.K_o)
     ws = _empty(need, torch.uint8, X.device, stream, scratch=True)
     Y = _empty((M, w.N), out_dtype, X.device, stream)

@@ -163,7 +163,7 @@ py::tuple gemm_q8(const at::Tensor &Xq, const OptTensor &s_x, const at::Tensor &
     return py::make_tuple(st, std::move(Y8));
 }
 
-// ---- fused endings, head norms and rotation: the checks of binding.py's _ending, _out, _rope, _norm_weight and _check_heads -----------------
+// ---- fused endings, head norms and rotation: the checks of binding.py's _layer, _array, _ending, _out, _rope, _norm_weight and _check_heads -----------------
 
 // The tensors are on the device that the call runs on.
 void on_device(int64_t device, std::initializer_list<const at::Tensor *> tensors)
@@ -189,6 +189,21 @@ void check_vector(const OptTensor &t, int64_t n, const char *what)
     if (t->scalar_type() != at::kFloat) throw py::type_error(std::string(what) + " must be float32");
     if (t->dim() != 1 || t->size(0) != n || (n > 1 && t->stride(0) != 1))
         throw py::value_error(std::string(what) + " must be a contiguous vector of " + std::to_string(n));
+}
+
+void check_array(const at::Tensor *t, int64_t n, at::ScalarType dtype, const char *what)
+{
+    if (t && t->scalar_type() != dtype) throw py::type_error(std::string(what) + " must be " + (dtype == at::kInt ? "int32" : "float32"));
+    if (t && (!t->is_contiguous() || t->numel() < n)) throw py::value_error(std::string(what) + " must be contiguous and hold " + std::to_string(n));
+}
+
+void check_layer(const at::Tensor &Wq, const at::Tensor *sn, const at::Tensor *so, const at::Tensor *perm, int64_t N, int64_t K)
+{
+    if (Wq.dim() != 2 || Wq.size(0) < N || (Wq.size(1) > 1 && Wq.stride(1) != 1))
+        throw py::value_error("the layer's Wq must have " + std::to_string(N) + " rows with unit inner stride");
+    check_array(sn, N, at::kFloat, "s_normal");
+    check_array(so, N, at::kFloat, "s_outlier");
+    check_array(perm, K, at::kInt, "perm");
 }
 
 qarvd_ending make_ending(int64_t M, int64_t N, int act, const OptTensor &gate, std::optional<int64_t> gate_rows, const OptTensor &residual,
@@ -228,11 +243,13 @@ py::tuple gemm_fused(const at::Tensor &Xq, const OptTensor &s_x, int bits, const
                      int64_t device)
 {
     const at::ScalarType out = Y ? Y->scalar_type() : c10::dtype_or_default(out_dtype);
+    check_layer(Wq, opt(sn), opt(so), nullptr, N, K);
     check_vector(bias, N, "bias");
     const qarvd_ending e = make_ending(M, N, act, gate, gate_rows, residual, out);
     const qarvd_dtype ydt = dtype_of(out);
-    on_device(device, {&Xq, opt(s_x), &Wq, opt(bias), opt(gate), opt(residual), opt(Y)});
-    if (Xq.dim() != 2 || Xq.size(0) < M) throw py::value_error("Xq has fewer than M rows");
+    on_device(device, {&Xq, opt(s_x), &Wq, opt(sn), opt(so), opt(bias), opt(gate), opt(residual), opt(Y)});
+    if (Xq.dim() != 2 || Xq.size(0) < M || (Xq.size(1) > 1 && Xq.stride(1) != 1)) throw py::value_error("Xq must have M rows with unit inner stride");
+    check_array(opt(s_x), M, at::kFloat, "s_x");
     if (Y) check_out(*Y, M, N, "Y");
     else Y = fresh({M, N}, out, Xq);
     const int st = run([&] {
@@ -251,10 +268,12 @@ py::tuple linear_fused(const at::Tensor &X, const OptTensor &perm, int bits, con
     const int64_t M = X.size(0);
     if (X.size(1) != K) throw py::value_error("X has " + std::to_string(X.size(1)) + " channels, the layer " + std::to_string(K));
     const at::ScalarType out = Y ? Y->scalar_type() : c10::dtype_or_default(out_dtype);
+    const at::Tensor *const order = K_o > 0 ? opt(perm) : nullptr;
+    check_layer(Wq, &sn, &so, order, N, K);
     check_vector(bias, N, "bias");
     const qarvd_ending e = make_ending(M, N, act, gate, gate_rows, residual, out);
     const qarvd_dtype xdt = dtype_of(X.scalar_type()), ydt = dtype_of(out);
-    on_device(device, {&X, &Wq, opt(bias), opt(gate), opt(residual), opt(Y)});
+    on_device(device, {&X, &Wq, &sn, &so, order, opt(bias), opt(gate), opt(residual), opt(Y)});
     if (Y) check_out(*Y, M, N, "Y");
     const size_t need = linear_workspace_fn((int32_t)M, (int32_t)K, (int32_t)K_o);
     const at::Tensor ws = fresh({(int64_t)need}, at::kByte, X);
@@ -354,6 +373,8 @@ py::tuple linear_qkv(const at::Tensor &X, const OptTensor &perm, int bits, const
     check_2d(X, "X");
     const int64_t M = X.size(0);
     if (X.size(1) != K) throw py::value_error("X has " + std::to_string(X.size(1)) + " channels, the layer " + std::to_string(K));
+    const at::Tensor *const order = K_o > 0 ? opt(perm) : nullptr;
+    check_layer(Wq, &sn, &so, order, N, K);
     check_vector(bias, N, "bias");
     check_norm_weight(wq, norm, heads_q, D, "weight_q");
     check_norm_weight(wk, norm, heads_k, D, "weight_k");
@@ -361,7 +382,7 @@ py::tuple linear_qkv(const at::Tensor &X, const OptTensor &perm, int bits, const
     const bool turn = make_rope(axes, freq, interleaved, pos, M, &r);
     const at::ScalarType out = c10::dtype_or_default(out_dtype);
     const qarvd_dtype xdt = dtype_of(X.scalar_type()), ydt = dtype_of(out);
-    on_device(device, {&X, &Wq, opt(bias), opt(wq), opt(wk), opt(pos), axes ? opt(freq) : nullptr});
+    on_device(device, {&X, &Wq, &sn, &so, order, opt(bias), opt(wq), opt(wk), opt(pos), axes ? opt(freq) : nullptr});
     const size_t need = linear_workspace_fn((int32_t)M, (int32_t)K, (int32_t)K_o);
     const at::Tensor ws = fresh({(int64_t)need}, at::kByte, X);
     at::Tensor Y = fresh({M, N}, out, X);
