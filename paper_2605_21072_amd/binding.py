@@ -572,7 +572,7 @@ def w8a8_dual_gemm_fused(Xq: torch.Tensor, s_x: torch.Tensor, w: DualScaleWeight
                                 variant, _stream(None), torch._C._cuda_getDevice())
         _check(st, "qarvd_dual_gemm_fused")
         return Y
-    dtype = out_dtype if Y is None else Y.dtype
+    dtype = Y.dtype if Y is not None else out_dtype or torch.get_default_dtype()
     _layer(w)
     _vector(bias, w.N, "bias")
     e = _ending(M, w.N, act, gate, gate_rows, residual, dtype)
@@ -603,7 +603,7 @@ def w8a8_linear_fused(X: torch.Tensor, w: DualScaleWeight, bias: Optional[torch.
     M, K = X.shape
     if K != w.K:
         raise ValueError("X has %d channels, the layer %d" % (K, w.K))
-    dtype = out_dtype if Y is None else Y.dtype
+    dtype = Y.dtype if Y is not None else out_dtype or torch.get_default_dtype()
     _layer(w)
     _vector(bias, w.N, "bias")
     e = _ending(M, w.N, act, gate, gate_rows, residual, dtype)
