@@ -1264,9 +1264,17 @@ void launch_rows(const RowsArgs &a, int cus, hipStream_t st)
 }
 
 template <int CH, int NT>
-void launch_rows_clip(const RowsArgs &a, hipStream_t st)
+void launch_rows_clip(RowsArgs a, hipStream_t st)
 {
-    hipLaunchKernelGGL((weight_rows_clip_kernel<CH, NT>), dim3(a.N), dim3(NT), 0, st, a);
+    // A launch has fewer than 2^32 work-items (of a count beyond, only the rest modulo 2^32 would run).
+    constexpr int32_t MOST = 1 << 22;
+    for (int32_t left = a.N; left > 0; left -= MOST) {
+        hipLaunchKernelGGL((weight_rows_clip_kernel<CH, NT>), dim3(left < MOST ? left : MOST), dim3(NT), 0, st, a);
+        a.W += (int64_t)MOST * a.ldw;
+        a.out += (int64_t)MOST * a.ldo;
+        a.s_normal += MOST;
+        a.s_outlier += MOST;
+    }
 }
 
 }  // namespace
