@@ -3,6 +3,7 @@
 
 Argument marshalling only: every step of the path runs in the HIP kernels of ``libqarvd.so``.
 There is no CPU or PyTorch fallback; a missing library raises at first use.
+Tensors are taken as data: results carry no autograd graph, and autograd does not see what is written in place.
 """
 from __future__ import annotations
 

@@ -288,6 +288,8 @@ __global__ __launch_bounds__(64 * WM * WN, (Geo2<BM, BN, WM, WN, NSTAGE, W4, (EN
     fetch_scales(lm0, ln0);
     issue(seq(0), 0);   // a fixed number of loads, so the wait the compiler puts before the scale writes covers
     park_scales(0);     // exactly the scale fetch and leaves the stage loads in flight
+    // (With a residual, 128 x 256 tiles and all general ones have a second wait, for all scales and gates, in front of the first stage load: va and vb come from a
+    // multiply-add whose unused 64-bit addend half shares a register with a load in flight.  The other builds have none.)
 #pragma unroll
     for (int p = 1; p < NSTAGE; ++p)
         if (p < T) issue(seq(p), p);
