@@ -95,7 +95,8 @@ int device_cus()
 
 struct Cand { int variant, bm, bn; double c, a, b; };
 
-int cheapest(const Cand *cand, int n, const GemmArgs &g)
+// `small`: up to how many times the output of two (64 x 64: one) rounds of 128 x 128 tiles the tiles of 64 rows are priced.
+int cheapest(const Cand *cand, int n, const GemmArgs &g, double small = 1.0)
 {
     const int cus = device_cus();      // rounds are counted over the CUs of the device the call runs on
     const double T = g.kp / 64;
@@ -104,7 +105,7 @@ int cheapest(const Cand *cand, int n, const GemmArgs &g)
     double best_cost = 1e300;
     for (int i = 0; i < n; ++i) {
         const Cand &c = cand[i];
-        if (c.bm == 64 && tiles128 > cus * c.bn / 64) continue;     // the small tiles only pay while 128x128 tiles leave CUs empty, or fill them badly
+        if (c.bm == 64 && tiles128 > small * cus * c.bn / 64) continue;     // the small tiles only pay while 128x128 tiles leave CUs empty, or fill them badly
         const long tiles = (long)((g.M + c.bm - 1) / c.bm) * ((g.N + c.bn - 1) / c.bn);
         const double cost = c.c + (double)((tiles + cus - 1) / cus) * (c.a + c.b * T);
         if (cost < best_cost) {
@@ -443,7 +444,8 @@ qarvd_status launch_fused(int bits, int32_t variant, const GemmArgs &g, qarvd_dt
         // aligned tiles of 128 rows: the 64-row tiles alone are the slower ones of a large product and not priced there (cheapest).  us, the best of them
         // and the any-width 128 x 128, groups of 100 tokens, bf16 residual: 4680 x 5120 -> 5120 187 and 148, 4680 x 13824 -> 5120 419 and 316, 4680 x 8960
         // -> 1536 96 and 69, 4680 x 1536 -> 1536 25.3 and 23.1.
-        const bool beside = bits == 4 || (g.last_group > 1 && g.gate_rows < 127);
+        // The 64-row tiles are priced a little further there: 1560 x 1536 -> 5120 in fp32, three rounds of 520 tiles, 31.4 and 38.1.
+        const bool short_groups = form == 0 && g.last_group > 1 && g.gate_rows < 127, beside = bits == 4 || short_groups;
         Cand cand[kNumFusedVariants];
         int n = 0;
         const bool gelu_alone = !g.gate && !g.R;
@@ -452,7 +454,7 @@ qarvd_status launch_fused(int bits, int32_t variant, const GemmArgs &g, qarvd_dt
             if ((v.BM * v.BN > 128 * 256 && !gelu_alone) || !gates_fit(v, g)) continue;
             if (v.bits == bits && (v.form == form || (beside && form == 0 && v.form == 1))) cand[n++] = {i + 1, v.BM, v.BN, v.c, v.a + (g.act == QARVD_ACT_GELU_TANH ? v.gelu : 0.0) + (gelu_alone ? 0.0 : v.res), v.b};
         }
-        variant = cheapest(cand, n, g);
+        variant = cheapest(cand, n, g, bits == 8 && short_groups ? 1.25 : 1.0);
     }
     const FusedVariant &v = kFusedVariants[variant - 1];
     if (v.bits != bits || (v.form == 0 && !(g.n_off <= 128 && g.vec_out)) || (v.form == 1 && !short_rows_ok(g)) || !grid_fits(v, g) || !gates_fit(v, g))

@@ -785,8 +785,8 @@ template <int BM, int BN, int WM, int WN, int NSTAGE, bool DUAL, bool DBG, typen
 qarvd_status launch128_one(const GemmArgs &g, hipStream_t st)
 {
     using G = Geo2<BM, BN, WM, WN, NSTAGE, W4, (END & ENDING_RESIDUAL) != 0>;
-    // (the tiles of 64 rows are not chosen for outputs that large: cheapest() leaves them out beyond two rounds of 128 x 128, 34 MB in fp32 on 256 CUs.  A dump
-    // of the accumulators is not timed)
+    // (the tiles of 64 rows are not chosen for outputs that large: cheapest() leaves them out beyond two and a half rounds of 128 x 128 tiles, 40 MB in fp32 on 256
+    // CUs.  A dump of the accumulators is not timed)
     if constexpr (WT && BM >= 128 && !DBG && sizeof(OutT) > 1)
         if (!output_writes_through(g, sizeof(OutT))) return launch128_one<BM, BN, WM, WN, NSTAGE, DUAL, DBG, OutT, GEN, W4, false, END>(g, st);
     auto k = gemm_dma128_kernel<BM, BN, WM, WN, NSTAGE, DUAL, DBG, OutT, GEN, W4, WT, END>;

@@ -46,3 +46,16 @@ def test_groups_too_short_for_the_tall_tiles(M, K, N, rows):
             pass
     chosen, *each = times([lambda v=v: call(v) for v in [0] + able])
     assert chosen <= 1.15 * min(each), (chosen, dict(zip(able, each)))
+
+
+def test_short_groups_where_tall_tiles_fill_badly():
+    """520 tiles of 128 x 128, three rounds on 256 CUs: 64-row tiles are priced beside them (without, 1.2 times the best kernel's time)."""
+    M, K, N, rows = 1560, 1536, 5120, 100
+    w, _ = layer(1, N, K, 64, 8)
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    X, R = torch.randn((M, K), generator=gen, device="cuda"), torch.randn((M, N), generator=gen, device="cuda")
+    gate = torch.randn((-(-M // rows), N), generator=gen, device="cuda")
+    Xq, s_x = q.quant_act(X, w.perm, 64)
+    Y = torch.empty_like(R)
+    chosen, *each = times([lambda v=v: q.w8a8_dual_gemm_fused(Xq, s_x, w, None, M, gate=gate, gate_rows=rows, residual=R, Y=Y, variant=v) for v in (0, 5, 6, 7, 8, 9)])
+    assert chosen <= 1.15 * min(each), (chosen, each)
